@@ -363,6 +363,87 @@ rc_status rc_maps_from_logits_noalloc(const void *logits, int32_t n_layers, int3
 rc_status rc_compact_mask(const uint8_t *mask, int32_t batch, int32_t tokens, int32_t *idx,
                           int32_t *offsets, int32_t *offsets_host, void *stream);
 
+/* 8-BIT OPERATORS.  Matrices, and keys and values of the cache, may be held as
+ * 8-bit floating-point numbers (e4m3: 4 exponent bits, 3 of mantissa, largest
+ * value 448, no infinity) in blocks that share a scale.  A scale is a power of
+ * two held as one byte e, 2^(e - 127), 1 <= e <= 254; a block that is all
+ * zeros may have any byte, so zeroed memory is a valid block of zeros.  The
+ * calls that write blocks choose the least e >= 1 with which the block's
+ * largest finite magnitude is at most 448 units, and round to nearest even;
+ * values that are not finite become NaN and do not count for the scale.
+ * These calls take no context.  They follow the conventions above: buffers
+ * belong to the caller, work goes to `stream` of the current device, nothing
+ * synchronises, nothing is kept between calls, and each may be captured into a
+ * graph. */
+
+/* A matrix [rows][cols] with a scale for each block_rows x 128 block:
+ * block_rows 1 for activations, 128 for weights.  Blocks at the right and
+ * lower edge are smaller where rows or cols end inside one. */
+typedef struct {
+  void *data;          /* device e4m3, rows `ld` bytes apart */
+  uint8_t *scales;     /* device: entry (column block j, row block i) is scales[j*scale_ld + i] */
+  int64_t ld;          /* a multiple of 16, >= cols */
+  int32_t rows, cols;  /* cols a multiple of 16, at most 65536 */
+  int32_t scale_ld;    /* a multiple of 16, >= row blocks */
+  int32_t block_rows;  /* 1 or 128 */
+} rc_qmat;
+
+/* Quantise x (device, rc_dtype dtype, rows `ldx` elements apart, ldx a multiple
+ * of 16 bytes) into `out`. */
+rc_status rc_quantize(const void *x, int32_t dtype, int64_t ldx, const rc_qmat *out, void *stream);
+
+/* out[m][n] = act(sum_k a[m][k] w[n][k] + bias[n]), a with block_rows 1, w with
+ * block_rows 128, equal cols.  act: tanh-approximated GELU if gelu is 1, none
+ * if 0.  bias: device float32 [w->rows], or NULL.  out: device, rc_dtype
+ * out_dtype, rows ldo >= w->rows elements apart.  Sums are float32; a bfloat16
+ * result is rounded once, and its sums of 128 products are exact to about 17
+ * bits; a float32 result has float32's precision throughout.  scratch: 16-byte
+ * aligned device memory of rc_qgemm_scratch_bytes(a->rows, w->rows, a->cols)
+ * bytes (may be NULL where that is 0); calls that may overlap in time need
+ * scratch of their own. */
+size_t rc_qgemm_scratch_bytes(int32_t m, int32_t n, int32_t k);
+rc_status rc_qgemm(const rc_qmat *a, const rc_qmat *w, const float *bias, int32_t gelu, void *out,
+                   int32_t out_dtype, int64_t ldo, void *scratch, size_t scratch_bytes, void *stream);
+
+/* Keys and values of `batch` chains in 8 bits (head dim 72), with a scale for
+ * each chain, head and block of 64 tokens, keys and values apart. */
+typedef struct {
+  void *data;            /* device e4m3; chain b at data + b*chain_stride: [heads][tokens/64][2][64][72],
+                            a block's 64 keys, then its 64 values */
+  uint8_t *scales;       /* device; chain b at scales + b*scale_stride: [heads][tokens/64][2] */
+  int64_t chain_stride;  /* bytes, a multiple of 16, at least heads*tokens*144 */
+  int64_t scale_stride;  /* bytes, at least heads*tokens/32 */
+  int32_t batch, heads;  /* heads at most 1024 */
+  int32_t tokens;        /* a multiple of 64, at most 2^24 */
+} rc_qcache;
+
+/* Merge the fresh keys and values of the active tokens into the cache: in every
+ * block that holds an active token the active rows are replaced, the others
+ * keep their values, and the block is stored with the scale of its merged
+ * contents (a kept value changes only where that makes it subnormal).  Other
+ * blocks are not written.  k, v: device, rc_dtype dtype, row r = active token r
+ * of the set (chains concatenated), heads side by side (heads*72), rows `ld`
+ * elements apart (a multiple of 16 bytes).  The set is as for rc_reuse_step; a
+ * block that is only partly active must hold valid contents (zeroed memory
+ * will do). */
+rc_status rc_qcache_store(const rc_qcache *cache, const rc_active_set *active, const void *k, const void *v,
+                          int32_t dtype, int64_t ld, void *stream);
+
+/* out[r] = sum_j p_j V_j / sum_j p_j, p_j = exp(scale q_r . K_j), for every head
+ * and every query row r of chain b, over keys j < key_len[b] of that chain.
+ * rows: the chains' row ranges (offsets and offsets_host; idx is not read, and
+ * the counts are not bounded by tokens).  key_len: device int32 [batch], clamped
+ * to 0 .. tokens, or NULL for all tokens; rows of a chain without keys are 0.
+ * What the cache holds behind key_len is not used, whatever it is.  q, out:
+ * device bfloat16, heads side by side, rows ldq / ldo elements apart
+ * (multiples of 8).  scratch: 16-byte aligned device memory of
+ * rc_qcache_attention_scratch_bytes(cache, rows) bytes (may be NULL where that
+ * is 0); calls that may overlap in time need scratch of their own. */
+size_t rc_qcache_attention_scratch_bytes(const rc_qcache *cache, const rc_active_set *rows);
+rc_status rc_qcache_attention(const rc_qcache *cache, const rc_active_set *rows, const int32_t *key_len,
+                              const void *q, int64_t ldq, float scale, void *out, int64_t ldo, void *scratch,
+                              size_t scratch_bytes, void *stream);
+
 /* Wait for `stream`; returns RC_ERR_HIP if any enqueued work failed. */
 rc_status rc_sync(void *stream);
 

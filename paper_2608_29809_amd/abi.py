@@ -76,6 +76,16 @@ class rc_step_io(C.Structure):
                 ("guidance_scale", C.c_float)]
 
 
+class rc_qmat(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_int64), ("rows", C.c_int32),
+                ("cols", C.c_int32), ("scale_ld", C.c_int32), ("block_rows", C.c_int32)]
+
+
+class rc_qcache(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scales", C.c_void_p), ("chain_stride", C.c_int64),
+                ("scale_stride", C.c_int64), ("batch", C.c_int32), ("heads", C.c_int32), ("tokens", C.c_int32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with paper_2608_29809_amd/build.py "
@@ -83,6 +93,7 @@ def _load():
     lib = C.CDLL(LIB_PATH)
     P, S, I32, U32 = C.c_void_p, C.c_size_t, C.c_int32, C.c_uint32
     pI32 = C.POINTER(C.c_int32)
+    I64, QM, QC, AS = C.c_int64, C.POINTER(rc_qmat), C.POINTER(rc_qcache), C.POINTER(rc_active_set)
     sig = {
         "rc_last_error": (C.c_char_p, []),
         "rc_create": (C.c_int, [C.POINTER(rc_model_config), C.POINTER(rc_weights), C.POINTER(P)]),
@@ -109,6 +120,12 @@ def _load():
         "rc_maps_from_logits": (C.c_int, [P, I32, I32, I32, I32, pI32, I32, P, P, S, P]),
         "rc_maps_from_logits_noalloc": (C.c_int, [P, I32, I32, I32, I32, pI32, I32, P, P]),
         "rc_compact_mask": (C.c_int, [P, I32, I32, P, P, pI32, P]),
+        "rc_quantize": (C.c_int, [P, I32, I64, QM, P]),
+        "rc_qgemm_scratch_bytes": (S, [I32, I32, I32]),
+        "rc_qgemm": (C.c_int, [QM, QM, P, I32, P, I32, I64, P, S, P]),
+        "rc_qcache_store": (C.c_int, [QC, AS, P, P, I32, I64, P]),
+        "rc_qcache_attention_scratch_bytes": (S, [QC, AS]),
+        "rc_qcache_attention": (C.c_int, [QC, AS, P, P, I64, C.c_float, P, I64, P, S, P]),
         "rc_sync": (C.c_int, [P]),
         "rc_set_kernel_timing": (C.c_int, [P, I32]),
         "rc_get_kernel_timing": (C.c_int, [P, I32, C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
@@ -147,7 +164,7 @@ def _wrap(name):
 for _n in ["rc_create", "rc_cache_offsets", "rc_cache_latent_offset", "rc_prepare_text", "rc_build_cache",
            "rc_reuse_step", "rc_update_cache", "rc_validate_active", "rc_reuse_step_hosted", "rc_build_cache_hosted",
            "rc_localize_region", "rc_maps_from_logits", "rc_maps_from_logits_noalloc", "rc_compact_mask", "rc_sync", "rc_set_kernel_timing",
-           "rc_get_kernel_timing"]:
+           "rc_get_kernel_timing", "rc_quantize", "rc_qgemm", "rc_qcache_store", "rc_qcache_attention"]:
     globals()[_n] = _wrap(_n)
 
 rc_destroy = LIB.rc_destroy
@@ -156,3 +173,5 @@ rc_text_kv_bytes = LIB.rc_text_kv_bytes
 rc_workspace_bytes = LIB.rc_workspace_bytes
 rc_staging_bytes = LIB.rc_staging_bytes
 rc_maps_from_logits_scratch_bytes = LIB.rc_maps_from_logits_scratch_bytes
+rc_qgemm_scratch_bytes = LIB.rc_qgemm_scratch_bytes
+rc_qcache_attention_scratch_bytes = LIB.rc_qcache_attention_scratch_bytes

@@ -17,6 +17,7 @@
 #include "rc_elem.h"
 #include "rc_launch.h"
 #include "rc_internal.h"
+#include "rc_quant.h"
 
 using rc::bf16;
 
@@ -797,6 +798,94 @@ rc_status static_scratch(void **out) {
   return RC_OK;
 }
 
+// ------------------------------------------------------------------ 8-bit operators
+
+rc_status check_qmat(const rc_qmat *m, const char *what) {
+  RC_CHECK(m, RC_ERR_INVALID_ARG, "%s is null", what);
+  RC_CHECK(m->rows >= 0 && m->cols >= 1, RC_ERR_SHAPE, "%s is %d x %d", what, m->rows, m->cols);
+  RC_CHECK(m->cols % 16 == 0 && m->cols <= rc::kQMaxCols, RC_ERR_UNSUPPORTED,
+           "%s has %d columns: a multiple of 16, at most %d", what, m->cols, rc::kQMaxCols);
+  RC_CHECK(m->block_rows == 1 || m->block_rows == rc::kQBlock, RC_ERR_UNSUPPORTED, "%s has blocks of %d rows, not 1 or %d",
+           what, m->block_rows, rc::kQBlock);
+  RC_CHECK(m->ld >= m->cols && m->ld <= (1 << 20), RC_ERR_SHAPE, "%s: rows of %d values are %lld bytes apart", what,
+           m->cols, (long long)m->ld);
+  RC_CHECK(m->ld % 16 == 0 && m->scale_ld % 16 == 0, RC_ERR_ALIGN, "%s: ld and scale_ld must be multiples of 16", what);
+  RC_CHECK(m->scale_ld >= (m->rows + m->block_rows - 1) / m->block_rows, RC_ERR_SHAPE,
+           "%s: scale_ld %d is less than its row blocks", what, m->scale_ld);
+  // (the grid of one launch)
+  RC_CHECK((long long)m->rows * ((m->cols + rc::kQBlock - 1) / rc::kQBlock) <= (1LL << 27), RC_ERR_SHAPE,
+           "%s is too large", what);
+  if (m->rows > 0) {
+    RC_CHECK(m->data && m->scales, RC_ERR_INVALID_ARG, "%s: a null pointer", what);
+    RC_CHECK(aligned16(m->data) && aligned16(m->scales), RC_ERR_ALIGN, "%s: not 16-byte aligned", what);
+  }
+  return RC_OK;
+}
+
+rc_status check_qcache(const rc_qcache *c) {
+  RC_CHECK(c, RC_ERR_INVALID_ARG, "cache is null");
+  RC_CHECK(c->data && c->scales, RC_ERR_INVALID_ARG, "a null pointer in the cache");
+  RC_CHECK(aligned16(c->data) && aligned16(c->scales), RC_ERR_ALIGN, "the cache is not 16-byte aligned");
+  RC_CHECK(c->batch >= 1 && c->batch <= 32767, RC_ERR_SHAPE, "cache batch %d out of range", c->batch);
+  RC_CHECK(c->heads >= 1 && c->heads <= 1024, RC_ERR_SHAPE, "heads %d outside [1, 1024]", c->heads);
+  RC_CHECK(c->tokens >= rc::kQTokens && c->tokens % rc::kQTokens == 0 && c->tokens <= (1 << 24), RC_ERR_UNSUPPORTED,
+           "tokens %d must be a positive multiple of %d, at most 2^24", c->tokens, rc::kQTokens);
+  RC_CHECK(c->batch == 1 || (c->chain_stride >= (int64_t)c->heads * c->tokens * 2 * rc::kHeadDim &&
+                             c->scale_stride >= (int64_t)c->heads * (c->tokens / rc::kQTokens) * 2),
+           RC_ERR_SHAPE, "the cache's chains overlap");
+  RC_CHECK(c->batch == 1 || c->chain_stride % 16 == 0, RC_ERR_ALIGN, "chain_stride must be a multiple of 16");
+  return RC_OK;
+}
+
+rc::QCacheArgs qcache_args(const rc_qcache *c) {
+  rc::QCacheArgs a{};
+  a.data = (uint8_t *)c->data;
+  a.scales = c->scales;
+  a.chain_stride = c->batch > 1 ? c->chain_stride : 0;
+  a.scale_chain_stride = c->batch > 1 ? c->scale_stride : 0;
+  a.heads = c->heads;
+  a.tokens = c->tokens;
+  return a;
+}
+
+// The row ranges of a set for a cache of `batch` chains: counts 0 .. most.
+rc_status check_rows(const rc_active_set *a, int batch, long long most) {
+  RC_CHECK(a, RC_ERR_INVALID_ARG, "active set is null");
+  RC_CHECK(a->batch == batch, RC_ERR_SHAPE, "active batch %d != cache batch %d", a->batch, batch);
+  RC_CHECK(a->offsets_host, RC_ERR_INVALID_ARG, "offsets_host is null");
+  RC_CHECK(a->offsets_host[0] == 0, RC_ERR_INDEX, "offsets_host[0] = %d != 0", a->offsets_host[0]);
+  for (int b = 0; b < batch; ++b) {
+    const long long n = (long long)a->offsets_host[b + 1] - a->offsets_host[b];
+    RC_CHECK(n >= 0 && n <= most, RC_ERR_INDEX, "chain %d has %lld rows, outside [0, %lld]", b, n, most);
+  }
+  RC_CHECK(a->offsets || a->offsets_host[batch] == 0, RC_ERR_INVALID_ARG, "offsets device array is null");
+  return RC_OK;
+}
+
+rc::ChainRows chain_rows_args(const rc_active_set *a) {
+  rc::ChainRows r{};
+  r.offsets = a->offsets;
+  r.n_arg = std::min(a->batch, rc::kQArgChains);
+  for (int b = 0; b <= r.n_arg; ++b) r.arg[b] = a->offsets_host[b];
+  return r;
+}
+
+constexpr int kMaxQRows = 1 << 24;  // query rows of one attention call
+
+rc::QAttnPlan qattention_plan(const rc_qcache *c, const rc_active_set *rows, int *max_rows) {
+  *max_rows = 0;
+  for (int b = 0; b < rows->batch; ++b) *max_rows = std::max(*max_rows, rows->offsets_host[b + 1] - rows->offsets_host[b]);
+  return rc::plan_qattention(rows->offsets_host, rows->batch, c->heads, c->tokens);
+}
+
+size_t qattention_part_bytes(const rc::QAttnPlan &p, long long rows, int heads) {
+  return p.splits == 1 ? 0 : align256((size_t)p.splits * rows * heads * rc::kHeadDim * sizeof(float));
+}
+
+size_t qattention_scratch(const rc::QAttnPlan &p, long long rows, int heads) {
+  return p.splits == 1 ? 0 : qattention_part_bytes(p, rows, heads) + (size_t)p.splits * rows * heads * 2 * sizeof(float);
+}
+
 }  // namespace
 
 // ====================================================================== C ABI
@@ -1184,6 +1273,120 @@ rc_status rc_compact_mask(const uint8_t *mask, int32_t batch, int32_t tokens, in
     RC_HIP(hipMemcpyAsync(offsets_host, offsets, sizeof(int32_t) * (batch + 1), hipMemcpyDeviceToHost, s));
     RC_HIP(hipStreamSynchronize(s));
   }
+  return RC_OK;
+}
+
+rc_status rc_quantize(const void *x, int32_t dtype, int64_t ldx, const rc_qmat *out, void *stream) {
+  g_err.clear();
+  RC_TRY(check_qmat(out, "out"));
+  RC_CHECK(dtype == RC_F32 || dtype == RC_BF16, RC_ERR_INVALID_ARG, "dtype %d unknown", dtype);
+  RC_CHECK(ldx >= out->cols, RC_ERR_SHAPE, "rows of %d values are %lld elements apart", out->cols, (long long)ldx);
+  RC_CHECK(ldx % (dtype == RC_F32 ? 4 : 8) == 0, RC_ERR_ALIGN, "ldx must be a multiple of 16 bytes");
+  if (out->rows == 0) return RC_OK;
+  RC_CHECK(x, RC_ERR_INVALID_ARG, "x is null");
+  RC_CHECK(aligned16(x), RC_ERR_ALIGN, "x not 16-byte aligned");
+  RC_CHECK(device_present(), RC_ERR_NO_DEVICE, "no HIP device");
+  rc::QuantArgs a{};
+  a.x = x; a.ldx = ldx; a.rows = out->rows; a.cols = out->cols;
+  a.q = (uint8_t *)out->data; a.ldq = out->ld; a.scales = out->scales; a.scale_ld = out->scale_ld;
+  RC_HIP(dtype == RC_F32 ? rc::launch_quantize<float>(a, out->block_rows, (hipStream_t)stream)
+                         : rc::launch_quantize<bf16>(a, out->block_rows, (hipStream_t)stream));
+  return RC_OK;
+}
+
+size_t rc_qgemm_scratch_bytes(int32_t m, int32_t n, int32_t k) {
+  if (m < 1 || n < 1 || k < 1) return 0;
+  return rc::qgemm_scratch(m, n, k);
+}
+
+rc_status rc_qgemm(const rc_qmat *a, const rc_qmat *w, const float *bias, int32_t gelu, void *out, int32_t out_dtype,
+                   int64_t ldo, void *scratch, size_t scratch_bytes, void *stream) {
+  g_err.clear();
+  RC_TRY(check_qmat(a, "a"));
+  RC_TRY(check_qmat(w, "w"));
+  RC_CHECK(a->block_rows == 1 && w->block_rows == rc::kQBlock, RC_ERR_UNSUPPORTED,
+           "a needs a scale for each row (block_rows 1), w for each %d (block_rows %d)", rc::kQBlock, rc::kQBlock);
+  RC_CHECK(a->cols == w->cols, RC_ERR_SHAPE, "a has %d columns, w %d", a->cols, w->cols);
+  RC_CHECK(w->rows >= 1, RC_ERR_SHAPE, "w has no rows");
+  RC_CHECK(gelu == 0 || gelu == 1, RC_ERR_INVALID_ARG, "gelu must be 0 or 1");
+  RC_CHECK(out_dtype == RC_F32 || out_dtype == RC_BF16, RC_ERR_INVALID_ARG, "out_dtype %d unknown", out_dtype);
+  RC_CHECK(ldo >= w->rows, RC_ERR_SHAPE, "rows of %d results are %lld elements apart", w->rows, (long long)ldo);
+  RC_CHECK(((long long)a->rows + 15) / 16 * (((long long)w->rows + 15) / 16) <= (1LL << 24), RC_ERR_SHAPE,
+           "%d x %d results are too many for one call", a->rows, w->rows);
+  RC_CHECK(!bias || (reinterpret_cast<uintptr_t>(bias) & 3u) == 0, RC_ERR_ALIGN, "bias not 4-byte aligned");
+  if (a->rows == 0) return RC_OK;
+  RC_CHECK(out, RC_ERR_INVALID_ARG, "out is null");
+  RC_CHECK(aligned16(out), RC_ERR_ALIGN, "out not 16-byte aligned");
+  const size_t need = rc::qgemm_scratch(a->rows, w->rows, a->cols);
+  RC_CHECK(scratch || need == 0, RC_ERR_INVALID_ARG, "scratch is null");
+  RC_CHECK(aligned16(scratch), RC_ERR_ALIGN, "scratch not 16-byte aligned");
+  RC_CHECK(scratch_bytes >= need, RC_ERR_CAPACITY, "scratch has %zu bytes, needs %zu", scratch_bytes, need);
+  RC_CHECK(device_present(), RC_ERR_NO_DEVICE, "no HIP device");
+  rc::QGemmArgs g{};
+  g.a = (const uint8_t *)a->data; g.as = a->scales; g.lda = a->ld; g.as_ld = a->scale_ld;
+  g.w = (const uint8_t *)w->data; g.ws = w->scales; g.ldw = w->ld; g.ws_ld = w->scale_ld;
+  g.M = a->rows; g.N = w->rows; g.K = a->cols; g.bias = bias; g.out = out; g.ldo = ldo;
+  g.scratch = (float *)scratch;
+  RC_HIP(rc::launch_qgemm(g, gelu != 0, out_dtype == RC_F32, (hipStream_t)stream));
+  return RC_OK;
+}
+
+rc_status rc_qcache_store(const rc_qcache *cache, const rc_active_set *active, const void *k, const void *v,
+                          int32_t dtype, int64_t ld, void *stream) {
+  g_err.clear();
+  RC_TRY(check_qcache(cache));
+  RC_TRY(check_rows(active, cache->batch, cache->tokens));
+  RC_CHECK(dtype == RC_F32 || dtype == RC_BF16, RC_ERR_INVALID_ARG, "dtype %d unknown", dtype);
+  RC_CHECK(ld >= (int64_t)cache->heads * rc::kHeadDim, RC_ERR_SHAPE, "rows of %d heads are %lld elements apart",
+           cache->heads, (long long)ld);
+  RC_CHECK(ld % (dtype == RC_F32 ? 4 : 8) == 0, RC_ERR_ALIGN, "ld must be a multiple of 16 bytes");
+  if (active->offsets_host[active->batch] == 0) return RC_OK;
+  RC_CHECK(active->idx && k && v, RC_ERR_INVALID_ARG, "idx, k or v is null");
+  RC_CHECK(aligned16(k) && aligned16(v), RC_ERR_ALIGN, "k/v not 16-byte aligned");
+  RC_CHECK(device_present(), RC_ERR_NO_DEVICE, "no HIP device");
+  rc::QStoreArgs a{};
+  a.c = qcache_args(cache); a.rows = chain_rows_args(active); a.idx = active->idx; a.k = k; a.v = v; a.ld = ld;
+  RC_HIP(dtype == RC_F32 ? rc::launch_qcache_store<float>(a, cache->batch, (hipStream_t)stream)
+                         : rc::launch_qcache_store<bf16>(a, cache->batch, (hipStream_t)stream));
+  return RC_OK;
+}
+
+size_t rc_qcache_attention_scratch_bytes(const rc_qcache *cache, const rc_active_set *rows) {
+  if (check_qcache(cache) != RC_OK || check_rows(rows, cache->batch, kMaxQRows) != RC_OK) return 0;
+  int max_rows = 0;
+  return qattention_scratch(qattention_plan(cache, rows, &max_rows), rows->offsets_host[rows->batch], cache->heads);
+}
+
+rc_status rc_qcache_attention(const rc_qcache *cache, const rc_active_set *rows, const int32_t *key_len, const void *q,
+                              int64_t ldq, float scale, void *out, int64_t ldo, void *scratch, size_t scratch_bytes,
+                              void *stream) {
+  g_err.clear();
+  RC_TRY(check_qcache(cache));
+  RC_TRY(check_rows(rows, cache->batch, kMaxQRows));
+  const int C = cache->heads * rc::kHeadDim, R = rows->offsets_host[rows->batch];
+  RC_CHECK(R <= kMaxQRows, RC_ERR_SHAPE, "%d query rows, at most %d", R, kMaxQRows);
+  RC_CHECK(ldq >= C && ldo >= C, RC_ERR_SHAPE, "rows of %d values are %lld and %lld elements apart", C, (long long)ldq,
+           (long long)ldo);
+  RC_CHECK(ldq % 8 == 0 && ldo % 8 == 0, RC_ERR_ALIGN, "ldq and ldo must be multiples of 8");
+  RC_CHECK(std::isfinite(scale), RC_ERR_INVALID_ARG, "scale is not finite");
+  if (R == 0) return RC_OK;
+  RC_CHECK(q && out, RC_ERR_INVALID_ARG, "q or out is null");
+  RC_CHECK(aligned16(q) && aligned16(out), RC_ERR_ALIGN, "q/out not 16-byte aligned");
+  RC_CHECK(!key_len || (reinterpret_cast<uintptr_t>(key_len) & 3u) == 0, RC_ERR_ALIGN, "key_len not 4-byte aligned");
+  int max_rows = 0;
+  const rc::QAttnPlan p = qattention_plan(cache, rows, &max_rows);
+  const size_t need = qattention_scratch(p, R, cache->heads);
+  RC_CHECK(scratch || need == 0, RC_ERR_INVALID_ARG, "scratch is null");
+  RC_CHECK(aligned16(scratch), RC_ERR_ALIGN, "scratch not 16-byte aligned");
+  RC_CHECK(scratch_bytes >= need, RC_ERR_CAPACITY, "scratch has %zu bytes, needs %zu", scratch_bytes, need);
+  RC_CHECK(device_present(), RC_ERR_NO_DEVICE, "no HIP device");
+  rc::QAttnArgs a{};
+  a.c = qcache_args(cache); a.rows = chain_rows_args(rows); a.key_len = key_len;
+  a.q = (const bf16 *)q; a.ldq = ldq; a.scale_log2 = (float)(scale * 1.4426950408889634); a.out = (bf16 *)out; a.ldo = ldo;
+  a.splits = p.splits; a.total_rows = R;
+  a.part = (float *)scratch;
+  a.ml = (float *)((char *)scratch + qattention_part_bytes(p, R, cache->heads));
+  RC_HIP(rc::launch_qattention(a, cache->batch, max_rows, (hipStream_t)stream));
   return RC_OK;
 }
 

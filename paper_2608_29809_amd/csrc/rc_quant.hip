@@ -1,0 +1,165 @@
+// Block quantisation to e4m3 with power-of-two scales, and the merge of fresh
+// keys and values into an 8-bit cache.
+#include "rc_common.h"
+#include "rc_launch.h"
+#include "rc_quant.h"
+
+namespace rc {
+
+template <typename T> __device__ __forceinline__ void q_load8(const T *p, float *v);
+template <> __device__ __forceinline__ void q_load8<float>(const float *p, float *v) {
+  const f32x4 a = *(const f32x4 *)p, b = *(const f32x4 *)(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = a[i];
+    v[4 + i] = b[i];
+  }
+}
+template <> __device__ __forceinline__ void q_load8<bf16>(const bf16 *p, float *v) {
+  const bf16x8 a = *(const bf16x8 *)p;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
+}
+
+// Maximum over the 16 lanes of a DPP row.
+__device__ __forceinline__ float row16_max(float v) {
+  v = fmaxf(v, dpp_mov<0xB1>(v));
+  v = fmaxf(v, dpp_mov<0x4E>(v));
+  v = fmaxf(v, dpp_mov<0x141>(v));
+  return fmaxf(v, dpp_mov<0x140>(v));
+}
+
+// A scale for each row and 128 columns: sixteen lanes take a block, eight
+// columns each.
+template <typename T> __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a, int cb) {
+  const long long unit = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int row = (int)(unit / cb), kb = (int)(unit - (long long)row * cb), l = threadIdx.x & 15;
+  if (row >= a.rows) return;
+  const int col = kb * kQBlock + l * 8;
+  float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  if (col < a.cols) q_load8<T>((const T *)a.x + row * a.ldx + col, v);
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, q_magnitude(v[i]));
+  const int e = q_exponent(row16_max(m));
+  const float inv = q_inverse(e);
+  if (col < a.cols) *(u32x2 *)(a.q + row * a.ldq + col) = u32x2{q_pack4(v, inv), q_pack4(v + 4, inv)};
+  if (l == 0) a.scales[(size_t)kb * a.scale_ld + row] = (uint8_t)e;
+}
+
+// A scale for each 128 x 128 tile: one workgroup each, 64 values per thread.
+template <typename T> __global__ __launch_bounds__(256) void quantize_tiles_kernel(QuantArgs a, int cb) {
+  __shared__ float red[4];
+  const int rb = blockIdx.x / cb, kb = blockIdx.x - rb * cb, tid = threadIdx.x;
+  const int col = kb * kQBlock + (tid & 15) * 8, row0 = rb * kQBlock + (tid >> 4);
+  float v[8][8], m = 0.0f;
+#pragma unroll
+  for (int p = 0; p < 8; ++p) {
+    const int row = row0 + p * 16;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[p][i] = 0.0f;
+    if (row < a.rows && col < a.cols) q_load8<T>((const T *)a.x + row * a.ldx + col, v[p]);
+  }
+#pragma unroll
+  for (int p = 0; p < 8; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, q_magnitude(v[p][i]));
+  m = wave_max(m);
+  if ((tid & 63) == 0) red[tid >> 6] = m;
+  __syncthreads();
+  const int e = q_exponent(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+  const float inv = q_inverse(e);
+#pragma unroll
+  for (int p = 0; p < 8; ++p) {
+    const int row = row0 + p * 16;
+    if (row < a.rows && col < a.cols)
+      *(u32x2 *)(a.q + row * a.ldq + col) = u32x2{q_pack4(v[p], inv), q_pack4(v[p] + 4, inv)};
+  }
+  if (tid == 0) a.scales[(size_t)kb * a.scale_ld + rb] = (uint8_t)e;
+}
+
+template <typename T> hipError_t launch_quantize(const QuantArgs &a, int block_rows, hipStream_t s) {
+  if (a.rows <= 0) return hipSuccess;
+  const int cb = (a.cols + kQBlock - 1) / kQBlock;
+  if (block_rows == 1) {
+    const long long units = (long long)a.rows * cb;
+    rc_launch(quantize_rows_kernel<T>, dim3((unsigned)((units + 15) / 16)), dim3(256), 0, s, a, cb);
+  } else {
+    rc_launch(quantize_tiles_kernel<T>, dim3((unsigned)((a.rows + kQBlock - 1) / kQBlock * cb)), dim3(256), 0, s, a, cb);
+  }
+  return hipGetLastError();
+}
+template hipError_t launch_quantize<bf16>(const QuantArgs &, int, hipStream_t);
+template hipError_t launch_quantize<float>(const QuantArgs &, int, hipStream_t);
+
+// ------------------------------------------------------------------ cache store
+
+// First position in [lo, hi) of an ascending list whose entry is >= key: the
+// wave probes 64 places at a time.
+__device__ __forceinline__ int wave_lower_bound(const int *idx, int lo, int hi, int key) {
+  const int lane = threadIdx.x & 63;
+  while (lo < hi) {
+    const int step = (hi - lo + 63) >> 6;  // places lo, lo + step, ...
+    const int at = lo + lane * step;
+    const unsigned long long less = __ballot(at < hi && idx[min(at, hi - 1)] < key);
+    const int n = __popcll(less);  // (ascending: the lanes below are the first n)
+    if (n == 0) return lo;
+    const int last = lo + (n - 1) * step;
+    lo = last + 1;
+    hi = min(hi, last + step);
+  }
+  return lo;
+}
+
+// One workgroup per chain, block of 64 tokens, head, and keys or values.  The
+// block's fresh rows take the places of their tokens, the others keep their
+// values; the scale is that of the merged block.
+template <typename T> __global__ __launch_bounds__(192) void qcache_store_kernel(QStoreArgs a) {
+  constexpr int CPR = kHeadDim / 8;  // chunks of eight values per token
+  __shared__ int row_of[kQTokens];
+  __shared__ float red[3];
+  const int tid = threadIdx.x, blk = blockIdx.x, head = blockIdx.y >> 1, which = blockIdx.y & 1, b = blockIdx.z;
+  const int2 rr = chain_rows(a.rows, b);
+  const int lo = wave_lower_bound(a.idx, rr.x, rr.y, blk * kQTokens);
+  const int hi = wave_lower_bound(a.idx, lo, min(rr.y, lo + kQTokens), (blk + 1) * kQTokens);
+  if (lo >= hi) return;
+  if (tid < kQTokens) row_of[tid] = -1;
+  __syncthreads();
+  if (tid < hi - lo) row_of[a.idx[lo + tid] & (kQTokens - 1)] = lo + tid;
+  __syncthreads();
+  const size_t tile = ((size_t)head * (a.c.tokens / kQTokens) + blk) * 2 + which;
+  uint8_t *data = a.c.data + b * a.c.chain_stride + tile * kQTileBytes;
+  uint8_t *scale = a.c.scales + b * a.c.scale_chain_stride + tile;
+  const T *src = (const T *)(which ? a.v : a.k) + head * kHeadDim;
+  const float old = q_factor(*scale);
+  float v[3][8], m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const int c = tid + i * 192, tok = c / CPR, d = (c - tok * CPR) * 8, r = row_of[tok];
+    if (r >= 0) {
+      q_load8<T>(src + r * a.ld + d, v[i]);
+    } else {
+      q_f32x8(*(const u32x2 *)(data + c * 8), old, v[i]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m = fmaxf(m, q_magnitude(v[i][k]));
+  }
+  m = wave_max(m);
+  if ((tid & 63) == 0) red[tid >> 6] = m;
+  __syncthreads();
+  const int e = q_exponent(fmaxf(fmaxf(red[0], red[1]), red[2]));
+  const float inv = q_inverse(e);
+#pragma unroll
+  for (int i = 0; i < 3; ++i) *(u32x2 *)(data + (tid + i * 192) * 8) = u32x2{q_pack4(v[i], inv), q_pack4(v[i] + 4, inv)};
+  if (tid == 0) *scale = (uint8_t)e;
+}
+
+template <typename T> hipError_t launch_qcache_store(const QStoreArgs &a, int chains, hipStream_t s) {
+  if (chains <= 0) return hipSuccess;
+  rc_launch(qcache_store_kernel<T>, dim3(a.c.tokens / kQTokens, 2 * a.c.heads, chains), dim3(192), 0, s, a);
+  return hipGetLastError();
+}
+template hipError_t launch_qcache_store<bf16>(const QStoreArgs &, int, hipStream_t);
+template hipError_t launch_qcache_store<float>(const QStoreArgs &, int, hipStream_t);
+
+}  // namespace rc

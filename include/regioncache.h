@@ -412,7 +412,7 @@ typedef struct {
                             a block's 64 keys, then its 64 values */
   uint8_t *scales;       /* device; chain b at scales + b*scale_stride: [heads][tokens/64][2] */
   int64_t chain_stride;  /* bytes, a multiple of 16, at least heads*tokens*144 */
-  int64_t scale_stride;  /* bytes, at least heads*tokens/32 */
+  int64_t scale_stride;  /* bytes, even, at least heads*tokens/32 */
   int32_t batch, heads;  /* heads at most 1024 */
   int32_t tokens;        /* a multiple of 64, at most 2^24 */
 } rc_qcache;

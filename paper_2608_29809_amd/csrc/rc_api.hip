@@ -833,7 +833,8 @@ rc_status check_qcache(const rc_qcache *c) {
   RC_CHECK(c->batch == 1 || (c->chain_stride >= (int64_t)c->heads * c->tokens * 2 * rc::kHeadDim &&
                              c->scale_stride >= (int64_t)c->heads * (c->tokens / rc::kQTokens) * 2),
            RC_ERR_SHAPE, "the cache's chains overlap");
-  RC_CHECK(c->batch == 1 || c->chain_stride % 16 == 0, RC_ERR_ALIGN, "chain_stride must be a multiple of 16");
+  RC_CHECK(c->batch == 1 || (c->chain_stride % 16 == 0 && c->scale_stride % 2 == 0), RC_ERR_ALIGN,
+           "chain_stride must be a multiple of 16, scale_stride of 2");
   return RC_OK;
 }
 
@@ -1386,7 +1387,7 @@ rc_status rc_qcache_attention(const rc_qcache *cache, const rc_active_set *rows,
   a.splits = p.splits; a.total_rows = R;
   a.part = (float *)scratch;
   a.ml = (float *)((char *)scratch + qattention_part_bytes(p, R, cache->heads));
-  RC_HIP(rc::launch_qattention(a, cache->batch, max_rows, (hipStream_t)stream));
+  RC_HIP(rc::launch_qattention(a, cache->batch, max_rows, p.qh, (hipStream_t)stream));
   return RC_OK;
 }
 

@@ -80,14 +80,16 @@ struct QAttnArgs {
   float scale_log2;         // softmax scale times log2(e)
   bf16 *out;
   long long ldo;
+  int chains;               // (set by launch_qattention)
   int splits;
   float *part;              // [splits][rows][heads * 72] (splits > 1)
   float *ml;                // [splits][rows][heads][2]: log2-domain reference and denominator
   int total_rows;
 };
-struct QAttnPlan { int splits; };
+constexpr int kQMaxSplits = 16;
+struct QAttnPlan { int qh, splits; };  // qh: 32-query halves per wave, or 0: 16 queries per workgroup
 QAttnPlan plan_qattention(const int *offsets, int chains, int heads, int tokens);
-hipError_t launch_qattention(const QAttnArgs &a, int chains, int max_rows, hipStream_t s);
+hipError_t launch_qattention(const QAttnArgs &a, int chains, int max_rows, int qh, hipStream_t s);
 
 // ------------------------------------------------------------------ device side
 

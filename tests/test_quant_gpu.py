@@ -326,25 +326,45 @@ def test_attention_large_logits(Q, rows, std):
     attention_case(Q, 1, 512, [rows], seed=9, std=std)
 
 
-@pytest.mark.parametrize("rows", [1, 70])
+# heads, tokens, rows: few queries without and with split keys, one and two query halves per wave likewise
+KERNELS = [(1, 256, 1), (1, 256, 70), (2, 4096, 5), (4, 192, 5000), (2, 4096, 1000), (9, 256, 7200), (16, 1856, 1300)]
+
+
+@pytest.mark.parametrize("heads,tokens,rows", KERNELS)
+def test_attention_kernels(Q, heads, tokens, rows):
+    attention_case(Q, heads, tokens, [rows], [tokens - 27], seed=rows)
+
+
+@pytest.mark.parametrize("heads,tokens,rows", KERNELS)
 @pytest.mark.parametrize("level", [-1.0, 1.0])
-def test_attention_logits_far_from_zero(Q, rows, level):
+def test_attention_logits_far_from_zero(Q, heads, tokens, rows, level):
     """Every logit of a query near -450, or +450: nothing may under- or overflow."""
-    cache, v, e, *_ = random_cache(Q, 1, 1, 4, seed=1)
+    cache, v, e, *_ = random_cache(Q, 1, heads, tokens // 64, seed=1)
     v[:, :, :, 0, :, 0], e[..., 0] = 128.0, 120
-    cache.data[:, :, :, 0, :, 0] = torch.full((1, 1, 4, 64), 128.0, device="cuda").to(torch.float8_e4m3fn)
+    cache.data[:, :, :, 0, :, 0] = torch.full((1, heads, tokens // 64, 64), 128.0, device="cuda").to(torch.float8_e4m3fn)
     cache.scales[..., 0] = 120
-    q = rnd(torch.bfloat16, rows, 72, seed=2, std=0.5)
-    q[:, 0] = 3840.0 * level
+    q = rnd(torch.bfloat16, rows, heads * 72, seed=2, std=0.5)
+    q[:, ::72] = 3840.0 * level
     o = Q.qcache_attention(cache, rows_set([rows]), dev(q, torch.bfloat16))
-    check_attention(o, v, e, [rows], [256], q)
+    check_attention(o, v, e, [rows], [tokens], q)
 
 
-@pytest.mark.parametrize("rows", [1, 33, 150])
+@pytest.mark.parametrize("heads,tokens,rows", KERNELS)
+def test_attention_large_values(Q, heads, tokens, rows):
+    """Values near the largest float beside large weights: only their weighted mean is finite."""
+    cache, v, e, *_ = random_cache(Q, 1, heads, tokens // 64, seed=1)
+    e[..., 0], e[..., 1] = 122, 240  # values up to 448 * 2^113 = 4.6e36
+    cache.scales.copy_(torch.from_numpy(e).to(torch.uint8))
+    q = rnd(torch.bfloat16, rows, heads * 72, seed=2, std=0.3)
+    o = Q.qcache_attention(cache, rows_set([rows]), dev(q, torch.bfloat16))
+    check_attention(o, v, e, [rows], [tokens], q)
+
+
+@pytest.mark.parametrize("heads,rows", [(2, 1), (2, 33), (2, 150), (4, 5000), (9, 7200)])
 @pytest.mark.parametrize("key_len", [0, 1, 70, 128, 200])
-def test_attention_ignores_what_lies_behind_the_keys(Q, rows, key_len):
+def test_attention_ignores_what_lies_behind_the_keys(Q, heads, rows, key_len):
     """NaN codes and scale bytes of 255 behind key_len."""
-    cache, v, e, *_ = random_cache(Q, 1, 2, 4, seed=key_len)
+    cache, v, e, *_ = random_cache(Q, 1, heads, 4, seed=key_len)
     e[..., 0] = 122
     cache.scales[..., 0] = 122
     raw = cache.data.view(torch.uint8)
@@ -354,20 +374,22 @@ def test_attention_ignores_what_lies_behind_the_keys(Q, rows, key_len):
         v[:, :, blk, :, n:] = 0.0
         if n == 0:
             cache.scales[:, :, blk] = 255
-    q = rnd(torch.bfloat16, rows, 144, seed=3, std=0.3)
+    q = rnd(torch.bfloat16, rows, heads * 72, seed=3, std=0.3)
     o = Q.qcache_attention(cache, rows_set([rows]), dev(q, torch.bfloat16),
                            key_len=torch.tensor([key_len], dtype=torch.int32, device="cuda"))
     check_attention(o, v, e, [rows], [key_len], q)
 
 
-def test_attention_nan_stays_in_its_chain_head_and_row(Q):
+@pytest.mark.parametrize("counts", [[4, 6], [9000, 2300]])
+def test_attention_nan_stays_in_its_chain_head_and_row(Q, counts):
     cache, v, e, *_ = random_cache(Q, 2, 2, 2, seed=1)
-    q = rnd(torch.bfloat16, 10, 144, seed=2, std=0.05)
-    q[7, 3] = np.nan                       # row 7 (chain 1), head 0
+    rows, last = sum(counts), counts[0] + 3
+    q = rnd(torch.bfloat16, rows, 144, seed=2, std=0.05)
+    q[last, 3] = np.nan                    # a row of chain 1, head 0
     cache.data[0, 1, 1, 1, 5, 8] = float("nan")  # chain 0, head 1: dim 8 of every row
-    o = np64(Q.qcache_attention(cache, rows_set([4, 6]), dev(q, torch.bfloat16)))
-    bad = np.zeros((10, 144), bool)
-    bad[7, :72], bad[:4, 72 + 8] = True, True
+    o = np64(Q.qcache_attention(cache, rows_set(counts), dev(q, torch.bfloat16)))
+    bad = np.zeros((rows, 144), bool)
+    bad[last, :72], bad[:counts[0], 72 + 8] = True, True
     np.testing.assert_array_equal(np.isnan(o), bad)
 
 

@@ -397,13 +397,9 @@ rc_status rc_quantize(const void *x, int32_t dtype, int64_t ldx, const rc_qmat *
  * if 0.  bias: device float32 [w->rows], or NULL.  out: device, rc_dtype
  * out_dtype, rows ldo >= w->rows elements apart.  Sums are float32; a bfloat16
  * result is rounded once, and its sums of 128 products are exact to about 17
- * bits; a float32 result has float32's precision throughout.  scratch: 16-byte
- * aligned device memory of rc_qgemm_scratch_bytes(a->rows, w->rows, a->cols)
- * bytes (may be NULL where that is 0); calls that may overlap in time need
- * scratch of their own. */
-size_t rc_qgemm_scratch_bytes(int32_t m, int32_t n, int32_t k);
+ * bits; a float32 result has float32's precision throughout. */
 rc_status rc_qgemm(const rc_qmat *a, const rc_qmat *w, const float *bias, int32_t gelu, void *out,
-                   int32_t out_dtype, int64_t ldo, void *scratch, size_t scratch_bytes, void *stream);
+                   int32_t out_dtype, int64_t ldo, void *stream);
 
 /* Keys and values of `batch` chains in 8 bits (head dim 72), with a scale for
  * each chain, head and block of 64 tokens, keys and values apart. */

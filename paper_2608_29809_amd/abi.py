@@ -121,8 +121,7 @@ def _load():
         "rc_maps_from_logits_noalloc": (C.c_int, [P, I32, I32, I32, I32, pI32, I32, P, P]),
         "rc_compact_mask": (C.c_int, [P, I32, I32, P, P, pI32, P]),
         "rc_quantize": (C.c_int, [P, I32, I64, QM, P]),
-        "rc_qgemm_scratch_bytes": (S, [I32, I32, I32]),
-        "rc_qgemm": (C.c_int, [QM, QM, P, I32, P, I32, I64, P, S, P]),
+        "rc_qgemm": (C.c_int, [QM, QM, P, I32, P, I32, I64, P]),
         "rc_qcache_store": (C.c_int, [QC, AS, P, P, I32, I64, P]),
         "rc_qcache_attention_scratch_bytes": (S, [QC, AS]),
         "rc_qcache_attention": (C.c_int, [QC, AS, P, P, I64, C.c_float, P, I64, P, S, P]),
@@ -173,5 +172,4 @@ rc_text_kv_bytes = LIB.rc_text_kv_bytes
 rc_workspace_bytes = LIB.rc_workspace_bytes
 rc_staging_bytes = LIB.rc_staging_bytes
 rc_maps_from_logits_scratch_bytes = LIB.rc_maps_from_logits_scratch_bytes
-rc_qgemm_scratch_bytes = LIB.rc_qgemm_scratch_bytes
 rc_qcache_attention_scratch_bytes = LIB.rc_qcache_attention_scratch_bytes

@@ -1295,13 +1295,8 @@ rc_status rc_quantize(const void *x, int32_t dtype, int64_t ldx, const rc_qmat *
   return RC_OK;
 }
 
-size_t rc_qgemm_scratch_bytes(int32_t m, int32_t n, int32_t k) {
-  if (m < 1 || n < 1 || k < 1) return 0;
-  return rc::qgemm_scratch(m, n, k);
-}
-
 rc_status rc_qgemm(const rc_qmat *a, const rc_qmat *w, const float *bias, int32_t gelu, void *out, int32_t out_dtype,
-                   int64_t ldo, void *scratch, size_t scratch_bytes, void *stream) {
+                   int64_t ldo, void *stream) {
   g_err.clear();
   RC_TRY(check_qmat(a, "a"));
   RC_TRY(check_qmat(w, "w"));
@@ -1318,17 +1313,12 @@ rc_status rc_qgemm(const rc_qmat *a, const rc_qmat *w, const float *bias, int32_
   if (a->rows == 0) return RC_OK;
   RC_CHECK(out, RC_ERR_INVALID_ARG, "out is null");
   RC_CHECK(aligned16(out), RC_ERR_ALIGN, "out not 16-byte aligned");
-  const size_t need = rc::qgemm_scratch(a->rows, w->rows, a->cols);
-  RC_CHECK(scratch || need == 0, RC_ERR_INVALID_ARG, "scratch is null");
-  RC_CHECK(aligned16(scratch), RC_ERR_ALIGN, "scratch not 16-byte aligned");
-  RC_CHECK(scratch_bytes >= need, RC_ERR_CAPACITY, "scratch has %zu bytes, needs %zu", scratch_bytes, need);
   RC_CHECK(device_present(), RC_ERR_NO_DEVICE, "no HIP device");
   rc::QGemmArgs g{};
   g.a = (const uint8_t *)a->data; g.as = a->scales; g.lda = a->ld; g.as_ld = a->scale_ld;
   g.w = (const uint8_t *)w->data; g.ws = w->scales; g.ldw = w->ld; g.ws_ld = w->scale_ld;
   g.M = a->rows; g.N = w->rows; g.K = a->cols; g.bias = bias; g.out = out; g.ldo = ldo;
-  g.scratch = (float *)scratch;
-  RC_HIP(rc::launch_qgemm(g, gelu != 0, out_dtype == RC_F32, (hipStream_t)stream));
+  RC_HIP(rc::launch_qgemm(g, rc::plan_qgemm(g.M, g.N, g.K), gelu != 0, out_dtype == RC_F32, (hipStream_t)stream));
   return RC_OK;
 }
 

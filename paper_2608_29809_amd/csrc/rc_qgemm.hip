@@ -10,9 +10,17 @@
 // float32 results: the operands become bfloat16 with their scales applied
 // (exactly), for 16x16x32 instructions whose sums keep float32's precision
 // (8e-8 of the result's norm over 36 blocks, as a float32 library product).
+//
+// W is operand A of the matrix instruction, so a lane's accumulators are four
+// consecutive columns of one row.  Lane (l16, lq) of an operand supplies, of
+// row l16, the 16-byte chunks lq and lq + 4 of the block's eight, in either
+// matrix (the order of K inside a block is free).
 #include "rc_common.h"
 #include "rc_launch.h"
 #include "rc_quant.h"
+
+#include <algorithm>
+#include <cmath>
 
 namespace rc {
 
@@ -21,140 +29,446 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kQMaxBlocks = kQMaxCols / kQBlock;
 
-// Workgroup tile of 16 FM WGM rows and 16 FN WGN columns.  W is operand A of
-// the matrix instruction, so a lane's accumulators are four consecutive
-// columns of one row.
-template <int FM, int FN, int WGM, int WGN, bool GELU, typename OUT>
-__global__ __launch_bounds__(64 * WGM * WGN) void qgemm_kernel(QGemmArgs g) {
-  constexpr int NW = WGM * WGN, BM = 16 * FM * WGM, BN = 16 * FN * WGN;
+template <int N> __device__ __forceinline__ void wait_vm_q() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// The products of one block of K: acc += w a, scale bytes ew (uniform) and ea.
+template <bool F32> __device__ __forceinline__ f32x4 q_mma(i32x8 w, i32x8 a, f32x4 acc, int ew, int ea) {
+  if constexpr (!F32) return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, acc, 0, 0, 0, ew, 0, ea);
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+        q_bf16x8(u32x2{(uint32_t)w[2 * q], (uint32_t)w[2 * q + 1]}, q_factor(ew)),
+        q_bf16x8(u32x2{(uint32_t)a[2 * q], (uint32_t)a[2 * q + 1]}, q_factor(ea)), acc, 0, 0, 0);
+  return acc;
+}
+
+template <typename OUT> __device__ __forceinline__ void q_store4(OUT *o, const f32x4 v, bool vec, int left) {
+  typedef OUT out4 __attribute__((ext_vector_type(4)));
+  if (vec && left >= 4) {
+    *(out4 *)o = out4{(OUT)v[0], (OUT)v[1], (OUT)v[2], (OUT)v[3]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < left) o[e] = (OUT)v[e];
+  }
+}
+
+// ------------------------------------------------------------------ few tiles
+
+// A workgroup's KG waves each take every KG-th block of K of the same tile of
+// 16 FM x 16 FN results, from memory to registers without LDS (no operand is
+// shared between waves), and their sums are joined in LDS in a fixed order.
+template <int FM, int FN, int KG, bool GELU, typename OUT>
+__global__ __launch_bounds__(64 * KG) void qgemm_split_kernel(QGemmArgs g) {
   constexpr bool F32 = sizeof(OUT) == 4;
-  constexpr int STAGE = (BM + BN) * kQBlock, TC = STAGE / 1024;  // wave copies of 1 KB: eight rows
-  static_assert(TC % NW == 0 && kQBlock % (16 * FN) == 0 && BM % 64 == 0, "tile");
-  constexpr int NL = TC / NW;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
-  __shared__ uint8_t sa[2][BM], sw[(BN + kQBlock - 1) / kQBlock][kQMaxBlocks];
+  constexpr int BM = 16 * FM, BN = 16 * FN, LD = BN + 4;
+  __shared__ __attribute__((aligned(16))) float part[KG * BM * LD];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave / WGN, wn = wave % WGN, l16 = lane & 15, lq = lane >> 4;
-  const int tiles_n = (g.N + BN - 1) / BN, L = xcd_logical_id(blockIdx.x, gridDim.x);
-  const int tm = L / tiles_n, tn = L - tm * tiles_n, m0 = tm * BM, n0 = tn * BN;
+  const int l16 = lane & 15, lq = lane >> 4;
+  const int tiles_m = (g.M + BM - 1) / BM, L = xcd_logical_id(blockIdx.x, gridDim.x);
+  const int tn = L / tiles_m, tm = L - tn * tiles_m, m0 = tm * BM, n0 = tn * BN;
   const int nk = (g.K + kQBlock - 1) / kQBlock;
+  const uint8_t *pa[FM], *pw[FN];
+  int ra[FM];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    ra[i] = min(m0 + i * 16 + l16, g.M - 1);
+    pa[i] = g.a + ra[i] * g.lda;
+  }
+#pragma unroll
+  for (int j = 0; j < FN; ++j) pw[j] = g.w + min(n0 + j * 16 + l16, g.N - 1) * g.ldw;
+  const uint8_t *ws = g.ws + n0 / kQBlock;  // (a tile's columns share their scales)
+  f32x4 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  struct Block {
+    i32x4 a[FM][2], w[FN][2];
+    int ea[FM], ew;
+  };
+  auto load = [&](Block &b, int kb) {
+    const int k0 = kb * kQBlock, c0 = min(k0 + lq * 16, g.K - 16), c1 = min(k0 + lq * 16 + 64, g.K - 16);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      b.w[j][0] = *(const i32x4 *)(pw[j] + c0);
+      b.w[j][1] = *(const i32x4 *)(pw[j] + c1);
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      b.a[i][0] = *(const i32x4 *)(pa[i] + c0);
+      b.a[i][1] = *(const i32x4 *)(pa[i] + c1);
+      b.ea[i] = g.as[(size_t)kb * g.as_ld + ra[i]];
+    }
+    b.ew = ws[(size_t)kb * g.ws_ld];
+  };
+  auto multiply = [&](Block &b, int kb) {
+    const int left = (g.K - kb * kQBlock) / 16;  // chunks of 16 that exist: zeros for the others
+    if (left < 8) {
+      const i32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        b.w[j][0] = lq < left ? b.w[j][0] : zero;
+        b.w[j][1] = lq + 4 < left ? b.w[j][1] : zero;
+      }
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        b.a[i][0] = lq < left ? b.a[i][0] : zero;
+        b.a[i][1] = lq + 4 < left ? b.a[i][1] : zero;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        acc[i][j] = q_mma<F32>(__builtin_shufflevector(b.w[j][0], b.w[j][1], 0, 1, 2, 3, 4, 5, 6, 7),
+                               __builtin_shufflevector(b.a[i][0], b.a[i][1], 0, 1, 2, 3, 4, 5, 6, 7), acc[i][j], b.ew, b.ea[i]);
+  };
+  Block b0, b1;
+  if (wave < nk) load(b0, wave);
+  for (int kb = wave; kb < nk; kb += 2 * KG) {
+    if (kb + KG < nk) load(b1, kb + KG);
+    multiply(b0, kb);
+    if (kb + KG >= nk) break;
+    if (kb + 2 * KG < nk) load(b0, kb + 2 * KG);
+    multiply(b1, kb + KG);
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) *(f32x4 *)(part + (wave * BM + i * 16 + l16) * LD + j * 16 + lq * 4) = acc[i][j];
+  __syncthreads();
+  OUT *out = (OUT *)g.out;
+  const bool vec = (g.ldo & 3) == 0;
+#pragma nounroll
+  for (int c = tid; c < BM * BN / 4; c += 64 * KG) {
+    const int r = c / (BN / 4), n = (c - r * (BN / 4)) * 4;
+    f32x4 v = *(const f32x4 *)(part + r * LD + n);
+#pragma unroll
+    for (int w = 1; w < KG; ++w) {
+      const f32x4 p = *(const f32x4 *)(part + (w * BM + r) * LD + n);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += p[e];
+    }
+    if (m0 + r >= g.M) break;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (g.bias) v[e] += g.bias[min(n0 + n + e, g.N - 1)];
+      if (GELU) v[e] = gelu_tanh(v[e]);
+    }
+    q_store4(out + (m0 + r) * g.ldo + n0 + n, v, vec, g.N - n0 - n);
+  }
+}
+
+// ------------------------------------------------------------------ many tiles
+
+// Wave tiles of 16 FM rows x 16 FN columns; WGM x WGN waves share a ring of S
+// stages of one block of K, KG such groups take every KG-th block each.
+// * Operands move global -> LDS by direct copies of 1 KB per wave, eight rows of
+//   128 bytes (stages of half a block, half rows, take as many requests: 137
+//   instead of 101 us for 16384 x 1152 x 4608); the 16-byte chunks of a row are
+//   swizzled so that a fragment read of 16 rows touches every bank once.
+// * KG = 1: a step waits for its stage, and the next ones' copies run beside its
+//   products; W fragments are read one ahead.  Two workgroups per CU cover each
+//   other's waits and epilogues.
+// * KG > 1, one wave per group, for few tiles: nothing but its own copies is
+//   waited for, a block's fragments are read while the block before is
+//   multiplied, in the registers that its fragments leave, and the groups' sums
+//   are joined in LDS in a fixed order.
+// What bounds it: for 16384 x 4608 x 1152 (128 x 128 tiles: 115 us, 132 with GELU;
+// 1.5 PFLOP/s at the 1.75 GHz that the power limit leaves) LDS, which gives 128
+// bytes per clock and takes 187 for 64 x 64 wave tiles with their copies, then
+// the epilogues.  256 x 256 tiles (64 x 128 per wave, 125 bytes per clock) have
+// one workgroup per CU: 111 and 133 us, and 128 instead of 105 at 16384 x 1152 x
+// 4608.  723 x 1152 x 4608 (64 x 64 tiles, KG = 4): 16 us, 34 with 128 x 128.
+template <int FM, int FN, int WGM, int WGN, int KG, int S, bool GELU, typename OUT>
+__global__ __launch_bounds__(64 * WGM * WGN * KG, 2) void qgemm_kernel(QGemmArgs g) {
+  constexpr int NG = WGM * WGN, NW = NG * KG, BM = 16 * FM * WGM, BN = 16 * FN * WGN;
+  static_assert(KG == 1 || NG == 1, "groups of one wave");
+  constexpr bool F32 = sizeof(OUT) == 4;
+  constexpr int STAGE = (BM + BN) * kQBlock, NL = STAGE / 1024 / NG, NA = BM * kQBlock / 1024 / NG;
+  static_assert(STAGE % (1024 * NG) == 0 && BM * kQBlock % (1024 * NG) == 0 && kQBlock % (16 * FN) == 0, "tile");
+  constexpr int NB = (BN + kQBlock - 1) / kQBlock;
+  constexpr int RING = KG * S * STAGE;
+  // results on their way out, float32: a band of 16 rows per wave, or every group's tile
+  constexpr int WN = 16 * FN, CLD = (KG == 1 ? WN : BN) + 4;
+  static_assert((KG == 1 ? NW * 16 : KG * BM) * CLD * 4 <= RING, "the results fit the ring");
+  __shared__ __attribute__((aligned(1024))) char lds[RING + KG * S * BM];
+  __shared__ uint8_t sw[NB][kQMaxBlocks];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __builtin_assume(wave >= 0 && wave < NW);
+  const int grp = wave / NG, wg = wave % NG, wm = wg / WGN, wn = wg % WGN, l16 = lane & 15, lq = lane >> 4;
+  const int tiles_m = (g.M + BM - 1) / BM, tiles_n = (g.N + BN - 1) / BN, L = xcd_logical_id(blockIdx.x, gridDim.x);
+  // bands of GM row tiles: the tiles in flight share rows and columns
+  constexpr int GM = 2048 / BM;
+  const int band0 = L / (GM * tiles_n), gm = min(GM, tiles_m - band0 * GM), idx = L - band0 * GM * tiles_n;
+  const int m0 = (band0 * GM + idx % gm) * BM, n0 = idx / gm * BN;
+  const int blocks = (g.K + kQBlock - 1) / kQBlock, tail = g.K - (blocks - 1) * kQBlock;
+  const int n = (blocks - grp + KG - 1) / KG;  // this group's: grp + KG i
 
   // rows past the last are clamped to it and never stored; columns of K past
   // the last are copies of its last 16 and multiplied as zeros
-  const uint8_t *src[NL];
-  int col[NL];
+  const int row8 = wg * 8 + (lane >> 3), chunk = ((lane & 7) ^ ((row8 >> 1) & 7)) * 16;
+  const uint8_t *a0 = g.a + m0 * g.lda, *w0 = g.w + n0 * g.ldw;
+  unsigned off[NL];
 #pragma unroll
-  for (int i = 0; i < NL; ++i) {
-    const int row = (i * NW + wave) * 8 + (lane >> 3);
-    col[i] = ((lane & 7) ^ ((row >> 1) & 7)) * 16;
-    src[i] = row < BM ? g.a + min(m0 + row, g.M - 1) * g.lda : g.w + min(n0 + row - BM, g.N - 1) * g.ldw;
-  }
-  auto issue = [&](int slot, int kt) {
+  for (int i = 0; i < NL; ++i)
+    off[i] = i < NA ? (unsigned)min(row8 + i * NG * 8, g.M - 1 - m0) * (unsigned)g.lda
+                    : (unsigned)min(row8 + (i - NA) * NG * 8, g.N - 1 - n0) * (unsigned)g.ldw;
+  char *ring = lds + grp * S * STAGE, *scales = lds + RING + grp * S * BM;
+  const unsigned ring0 = lds_address(ring) + wg * 1024, scales0 = lds_address(scales);
+  // (row scales: 16 a lane, by the group's first wave; their rows are padded to 16)
+  const unsigned sc_off = (unsigned)min(lane * 16, g.as_ld - 16 - m0);
+  auto issue = [&](int slot, int i) {
+    const int kb = grp + KG * i;
 #pragma unroll
-    for (int i = 0; i < NL; ++i)
-      lds_dma16(src[i] + min(kt * kQBlock + col[i], g.K - 16), lds + slot * STAGE + (i * NW + wave) * 1024);
+    for (int q = 0; q < NL; ++q) {
+      unsigned c = NG == 1 && (q & 1) ? chunk ^ 64 : chunk;  // (rows 8 further: the other half of the swizzle)
+      if (kb == blocks - 1) c = min((int)c, tail - 16);
+      lds_dma16s((q < NA ? a0 : w0) + (size_t)kb * kQBlock, off[q] + c, ring0 + slot * STAGE + q * NG * 1024);
+    }
+    if (wg == 0 && lane < BM / 16) lds_dma16s(g.as + (size_t)kb * g.as_ld + m0, sc_off, scales0 + slot * BM);
   };
-  auto row_scales = [&](int slot, int kt) {
-    for (int r = tid; r < BM; r += 64 * NW) sa[slot][r] = g.as[(size_t)kt * g.as_ld + min(m0 + r, g.M - 1)];
+  auto wait_blocks = [&](int later) {  // at most `later` younger blocks' copies are in flight
+    if (S > 2 && later >= 2) {
+      if (wg == 0) wait_vm_q<2 * NL + 2>();
+      else wait_vm_q<2 * NL>();
+    } else if (later >= 1) {
+      if (wg == 0) wait_vm_q<NL + 1>();
+      else wait_vm_q<NL>();
+    } else {
+      wait_vm_q<0>();
+    }
   };
-  for (int i = tid; i < nk; i += 64 * NW)
+  for (int i = tid; i < blocks; i += 64 * NW)
 #pragma unroll
-    for (int j = 0; j < (BN + kQBlock - 1) / kQBlock; ++j)
-      sw[j][i] = g.ws[(size_t)i * g.ws_ld + min(n0 / kQBlock + j, (g.N - 1) / kQBlock)];
+    for (int j = 0; j < NB; ++j) sw[j][i] = g.ws[(size_t)i * g.ws_ld + min(n0 / kQBlock + j, (g.N - 1) / kQBlock)];
+  __syncthreads();
 
   f32x4 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int fr = l16 * kQBlock, sz = (l16 >> 1) & 7;
-  auto frag = [&](const char *tile, int block, int kt) {
-    const char *p = tile + block * 16 * kQBlock + fr;
-    i32x4 lo = *(const i32x4 *)(p + ((lq ^ sz) << 4)), hi = *(const i32x4 *)(p + (((lq + 4) ^ sz) << 4));
-    if (kt * kQBlock + kQBlock > g.K) {
-      const int left = (g.K - kt * kQBlock) / 16;  // chunks of 16 that exist
-      if (lq >= left) lo = i32x4{0, 0, 0, 0};
-      if (lq + 4 >= left) hi = i32x4{0, 0, 0, 0};
+  const int sz = (l16 >> 1) & 7, c_lo = l16 * kQBlock + ((lq ^ sz) << 4), c_hi = l16 * kQBlock + (((lq + 4) ^ sz) << 4);
+  constexpr int RW = KG > 1 ? FN : 2;  // W fragments held
+  i32x8 a[FM], w[RW];
+  int ea[FM];
+  auto frag = [&](const char *rows, bool last) {
+    i32x4 lo = *(const i32x4 *)(rows + c_lo), hi = *(const i32x4 *)(rows + c_hi);
+    if (last) {
+      if (lq >= tail / 16) lo = i32x4{0, 0, 0, 0};
+      if (lq + 4 >= tail / 16) hi = i32x4{0, 0, 0, 0};
     }
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
+  auto read_a = [&](int slot, int i, bool last) {
+    a[i] = frag(ring + slot * STAGE + (wm * FM + i) * 16 * kQBlock, last);
+    ea[i] = *(const uint8_t *)(scales + slot * BM + (wm * FM + i) * 16 + l16);
+  };
+  auto read_w = [&](int slot, int j, bool last) { w[j % RW] = frag(ring + slot * STAGE + (BM + wn * WN + j * 16) * kQBlock, last); };
 
-  issue(0, 0);
-  row_scales(0, 0);
-  for (int kt = 0; kt < nk; ++kt) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (kt + 1 < nk) {
-      issue((kt + 1) & 1, kt + 1);
-      row_scales((kt + 1) & 1, kt + 1);
+  if constexpr (KG > 1) {
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+      if (i < n) issue(i, i);
+    wait_blocks(min(n - 1, S - 1));
+    const bool last0 = grp == blocks - 1 && tail < kQBlock;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) read_a(0, i, last0);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) read_w(0, j, last0);
+    int slot = 0;
+#pragma nounroll
+    for (int i = 0; i < n; ++i) {
+      const int kb = grp + KG * i, ns = slot == S - 1 ? 0 : slot + 1;
+      const int ew = sw[wn * WN / kQBlock][kb];
+      if (i + 1 < n) {
+        wait_blocks(min(n - 2 - i, S - 2));
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (i + S < n) issue(slot, i + S);
+      }
+      // (the last step's reads of a stale slot are never used)
+      const bool last = kb + KG == blocks - 1 && tail < kQBlock;
+      __builtin_amdgcn_sched_barrier(0);
+      constexpr int JT = FN > 2 ? FN - 2 : 1;  // from this column block on, row by row
+#pragma unroll
+      for (int j = 0; j < JT; ++j) {
+#pragma unroll
+        for (int q = 0; q < FM; ++q) acc[q][j] = q_mma<F32>(w[j], a[q], acc[q][j], ew, ea[q]);
+        read_w(ns, j, last);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int q = 0; q < FM; ++q) {
+#pragma unroll
+        for (int j = JT; j < FN; ++j) acc[q][j] = q_mma<F32>(w[j], a[q], acc[q][j], ew, ea[q]);
+        read_a(ns, q, last);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int j = JT; j < FN; ++j) read_w(ns, j, last);
+      __builtin_amdgcn_sched_barrier(0);
+      slot = ns;
     }
-    const char *st = lds + (kt & 1) * STAGE;
-    const int ew = sw[wn * FN * 16 / kQBlock][kt];
-    i32x8 w[FN];
+  } else {
 #pragma unroll
-    for (int j = 0; j < FN; ++j) w[j] = frag(st + BM * kQBlock, wn * FN + j, kt);
+    for (int i = 0; i < S - 1; ++i)
+      if (i < n) issue(i, i);
+    int slot = 0;
+#pragma nounroll
+    for (int i = 0; i < n; ++i) {
+      wait_blocks(min(n - 1 - i, S - 2));
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (i + S - 1 < n) issue(slot == 0 ? S - 1 : slot - 1, i + S - 1);
+      const bool last = i == blocks - 1 && tail < kQBlock;
+      const int ew = sw[wn * WN / kQBlock][i];
+      read_w(slot, 0, last);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const i32x8 a = frag(st, wm * FM + i, kt);
-      const int ea = sa[kt & 1][(wm * FM + i) * 16 + l16];
-      if constexpr (!F32) {
+      for (int q = 0; q < FM; ++q) read_a(slot, q, last);
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j], a, acc[i][j], 0, 0, 0, ew, 0, ea);
-      } else {
+      for (int j = 0; j < FN; ++j) {
+        if (j + 1 < FN) read_w(slot, j + 1, last);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const bf16x8 av = q_bf16x8(u32x2{(uint32_t)a[2 * q], (uint32_t)a[2 * q + 1]}, q_factor(ea));
+        for (int q = 0; q < FM; ++q) acc[q][j] = q_mma<F32>(w[j & 1], a[q], acc[q][j], ew, ea[q]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      slot = slot == S - 1 ? 0 : slot + 1;
+    }
+  }
+
+  // The results pass through LDS so that WN / 8 lanes (or BN / 8) store a row's
+  // columns and the code is a short loop (run once, each instruction of it is
+  // fetched from memory).
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  // Rows that are a multiple of 16 bytes apart: eight columns a lane.  Others:
+  // one column a lane, so that a store covers whole lines all the same.
+  float *res = (float *)lds;
+  constexpr int ROWS = KG == 1 ? 16 : BM, COLS = KG == 1 ? WN : BN, WHO = KG == 1 ? 64 : 64 * KG;
+  const int who = KG == 1 ? lane : tid, col0 = n0 + (KG == 1 ? wn * WN : 0);
+  OUT *out = (OUT *)g.out;
+  const bool vec = (g.ldo & 7) == 0;
+  const int c8 = vec ? who % (COLS / 8) * 8 : who % COLS, col = col0 + c8;
+  float bias[8];
 #pragma unroll
-          for (int j = 0; j < FN; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                q_bf16x8(u32x2{(uint32_t)w[j][2 * q], (uint32_t)w[j][2 * q + 1]}, q_factor(ew)), av, acc[i][j], 0, 0, 0);
+  for (int e = 0; e < 8; ++e) bias[e] = g.bias ? g.bias[min(col + e, g.N - 1)] : 0.0f;
+  // rows row0 .. + ROWS of the result from `tile`, the groups' sums joined in order
+  auto put = [&](const float *tile, int row0) {
+    if (vec) {
+#pragma nounroll
+      for (int r = who / (COLS / 8); r < ROWS; r += WHO / (COLS / 8)) {
+        float v[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          f32x4 x = *(const f32x4 *)(tile + r * CLD + c8 + 4 * h);
+#pragma unroll
+          for (int q = 1; q < KG; ++q) {
+            const f32x4 y = *(const f32x4 *)(tile + (q * BM + r) * CLD + c8 + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] += y[e];
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[4 * h + e] = x[e] + bias[4 * h + e];
+            if (GELU) v[4 * h + e] = gelu_tanh(v[4 * h + e]);
+          }
+        }
+        if (row0 + r >= g.M) break;
+        OUT *o = out + (row0 + r) * g.ldo + col;
+        if (col + 8 <= g.N) {
+          if constexpr (F32) {
+            *(f32x4 *)o = f32x4{v[0], v[1], v[2], v[3]};
+            *(f32x4 *)(o + 4) = f32x4{v[4], v[5], v[6], v[7]};
+          } else {
+            *(bf16x8 *)o = bf16x8{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3], (bf16)v[4], (bf16)v[5], (bf16)v[6], (bf16)v[7]};
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (col + e < g.N) o[e] = (OUT)v[e];
         }
       }
-    }
-  }
-
-  OUT *out = (OUT *)g.out;
-  const bool vec = (g.ldo & 3) == 0;
+    } else {
+#pragma nounroll
+      for (int r = who / COLS; r < ROWS; r += WHO / COLS) {
+        float v = tile[r * CLD + c8];
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const int m = m0 + (wm * FM + i) * 16 + l16;
-    if (m >= g.M) continue;
-#pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      const int n = n0 + (wn * FN + j) * 16 + lq * 4;
-      f32x4 v = acc[i][j];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (g.bias) v[e] += g.bias[min(n + e, g.N - 1)];
-        if (GELU) v[e] = gelu_tanh(v[e]);
-      }
-      OUT *o = out + m * g.ldo + n;
-      typedef OUT out4 __attribute__((ext_vector_type(4)));
-      if (vec && n + 3 < g.N) {
-        *(out4 *)o = out4{(OUT)v[0], (OUT)v[1], (OUT)v[2], (OUT)v[3]};
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n + e < g.N) o[e] = (OUT)v[e];
+        for (int q = 1; q < KG; ++q) v += tile[(q * BM + r) * CLD + c8];
+        v += bias[0];
+        if (GELU) v = gelu_tanh(v);
+        if (row0 + r < g.M && col < g.N) out[(row0 + r) * g.ldo + col] = (OUT)v;
       }
     }
+  };
+  if constexpr (KG == 1) {
+    float *band = res + wave * 16 * CLD;
+#pragma nounroll
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+      for (int q = 0; q < FM; ++q)
+        if (i == q)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) *(f32x4 *)(band + l16 * CLD + j * 16 + lq * 4) = acc[q][j];
+      put(band, m0 + (wm * FM + i) * 16);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) *(f32x4 *)(res + (grp * BM + i * 16 + l16) * CLD + j * 16 + lq * 4) = acc[i][j];
+    __syncthreads();
+    put(res, m0);
   }
 }
 
-template <bool GELU, typename OUT> static void launch_qg(const QGemmArgs &a, hipStream_t s) {
-  constexpr int BM = 128, BN = 128;
-  const long long tiles = (long long)((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN);
-  rc_launch(qgemm_kernel<4, 4, 2, 2, GELU, OUT>, dim3((unsigned)tiles), dim3(256), 0, s, a);
+template <bool GELU, typename OUT> static void launch_qg(const QGemmArgs &a, const QGemmPlan &p, hipStream_t s) {
+  const unsigned tiles = (unsigned)(((long long)a.M + p.bm - 1) / p.bm * ((a.N + p.bn - 1) / p.bn));
+#define RC_QG_SPLIT(FM, FN, KG) rc_launch(qgemm_split_kernel<FM, FN, KG, GELU, OUT>, dim3(tiles), dim3(64 * KG), 0, s, a)
+#define RC_QG(FM, FN, WGM, WGN, KG, S) \
+  rc_launch(qgemm_kernel<FM, FN, WGM, WGN, KG, S, GELU, OUT>, dim3(tiles), dim3(64 * WGM * WGN * KG), 0, s, a)
+  switch (p.bm * 1000 + p.bn) {
+    case 16016: (void)RC_QG_SPLIT(1, 1, 8); break;
+    case 32032: (void)RC_QG_SPLIT(2, 2, 8); break;
+    case 64032: (void)RC_QG(4, 2, 1, 1, 4, 3); break;
+    case 64064: (void)RC_QG(4, 4, 1, 1, 4, 2); break;
+    case 64128: (void)RC_QG(4, 2, 1, 4, 1, 3); break;
+    case 128128: (void)RC_QG(4, 4, 2, 2, 1, 2); break;
+  }
+#undef RC_QG
+#undef RC_QG_SPLIT
 }
 
-size_t qgemm_scratch(int, int, int) { return 0; }
+// The tile with the least estimated time: 5 us of ends, and for each step of K
+// the time of the workgroups that share a CU.  Measured, us: 1 x 4608 x 1152 6.5
+// (16 x 16), 64 x 4608 x 1152 7.4 (64 x 32; 32 x 32 8.9), 219 x 1000 x 1072 in
+// float32 6.6 (32 x 32; 64 x 32 8.1), 154 x 1152 x 4608 11.6 (64 x 32; 32 x 32
+// 13.0), 723 x 1152 x 4608 16.0 (64 x 64; 64 x 32 21), 723 x 4608 x 1152 14.0 (64 x
+// 128; 128 x 128 14.9, 64 x 64 26), 2458 x 4608 x 1152 30 (128 x 128; 64 x 128 35).
+QGemmPlan plan_qgemm(int M, int N, int K) {
+  struct Tile { int bm, bn, kg; double fixed, per; };  // us a step, and a step per workgroup of a CU
+  static constexpr Tile tiles[] = {{16, 16, 8, 0.0, 0.6}, {32, 32, 8, 0.0, 1.2}, {64, 32, 4, 0.0, 0.8},
+                                   {64, 64, 4, 0.0, 1.25}, {64, 128, 1, 0.15, 0.5}, {128, 128, 1, 0.3, 0.8}};
+  const int blocks = (K + kQBlock - 1) / kQBlock;
+  QGemmPlan best{128, 128};
+  double best_us = 1e30;
+  for (const Tile &t : tiles) {
+    const double wgs = std::ceil((double)M / t.bm) * std::ceil((double)N / t.bn) / 256;
+    const double load = t.kg > 1 ? std::ceil(wgs) : std::max(wgs, 1.0), steps = (blocks + t.kg - 1) / t.kg;
+    const double us = 5.0 + steps * (t.fixed + t.per * load);
+    if (us < best_us) {
+      best_us = us;
+      best = QGemmPlan{t.bm, t.bn};
+    }
+  }
+  return best;
+}
 
-hipError_t launch_qgemm(const QGemmArgs &a, bool gelu, bool f32_out, hipStream_t s) {
+hipError_t launch_qgemm(const QGemmArgs &a, const QGemmPlan &p, bool gelu, bool f32_out, hipStream_t s) {
   if (a.M <= 0) return hipSuccess;
   if (a.K > kQMaxBlocks * kQBlock || a.K % 16) return hipErrorInvalidValue;
-  if (f32_out) gelu ? launch_qg<true, float>(a, s) : launch_qg<false, float>(a, s);
-  else gelu ? launch_qg<true, bf16>(a, s) : launch_qg<false, bf16>(a, s);
+  if (f32_out) gelu ? launch_qg<true, float>(a, p, s) : launch_qg<false, float>(a, p, s);
+  else gelu ? launch_qg<true, bf16>(a, p, s) : launch_qg<false, bf16>(a, p, s);
   return hipGetLastError();
 }
 

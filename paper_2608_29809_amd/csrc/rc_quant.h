@@ -40,10 +40,10 @@ struct QGemmArgs {
   const float *bias;        // [N] or null
   void *out;
   long long ldo;            // elements
-  float *scratch;           // qgemm_scratch bytes
 };
-size_t qgemm_scratch(int M, int N, int K);
-hipError_t launch_qgemm(const QGemmArgs &a, bool gelu, bool f32_out, hipStream_t s);
+struct QGemmPlan { int bm, bn; };  // workgroup tile
+QGemmPlan plan_qgemm(int M, int N, int K);
+hipError_t launch_qgemm(const QGemmArgs &a, const QGemmPlan &p, bool gelu, bool f32_out, hipStream_t s);
 
 struct QCacheArgs {
   uint8_t *data;            // [heads][tokens / 64][2][64][72] per chain: keys, then values, of a block

@@ -156,10 +156,8 @@ def qgemm(a: QuantMatrix, w: QuantMatrix, bias: Optional[torch.Tensor] = None, g
     ldo = _rows(out, n, "out")
     _on_gpu(a.data, w.data, bias, out)
     if m:
-        nbytes = abi.rc_qgemm_scratch_bytes(m, n, a.data.shape[1])
-        scratch = torch.empty(nbytes, dtype=torch.uint8, device=out.device) if nbytes else None
         _call(abi.rc_qgemm, out.device, C.byref(a.struct()), C.byref(w.struct()), None if bias is None else bias.data_ptr(),
-              1 if gelu else 0, out.data_ptr(), _dtype(out, "out"), ldo, scratch.data_ptr() if nbytes else None, nbytes)
+              1 if gelu else 0, out.data_ptr(), _dtype(out, "out"), ldo)
     return out
 
 

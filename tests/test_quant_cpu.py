@@ -45,10 +45,10 @@ def test_matrix_refusals(over, status):
     assert abi.LIB.rc_quantize(FAKE, abi.RC_BF16, 256, C.byref(bad), None) == status
     assert abi.rc_last_error()
     if over.get("block_rows", 1) == 1:
-        assert abi.LIB.rc_qgemm(C.byref(bad), C.byref(w), None, 0, FAKE, 1, 40, FAKE, 1 << 40, None) in (status, -2)
+        assert abi.LIB.rc_qgemm(C.byref(bad), C.byref(w), None, 0, FAKE, 1, 40, None) in (status, -2)
     if "scale_ld" not in over:
         over = dict(block_rows=128, **{k: v for k, v in over.items() if k != "block_rows"})
-        assert abi.LIB.rc_qgemm(C.byref(a), C.byref(qmat(**over)), None, 0, FAKE, 1, 1 << 31, FAKE, 1 << 40, None) < 0
+        assert abi.LIB.rc_qgemm(C.byref(a), C.byref(qmat(**over)), None, 0, FAKE, 1, 1 << 31, None) < 0
 
 
 def test_quantize_refusals():
@@ -65,9 +65,9 @@ def test_quantize_refusals():
 
 
 def test_qgemm_refusals():
-    def call(a=None, w=None, bias=FAKE, gelu=0, out=FAKE, dt=1, ldo=40, scratch=FAKE, nbytes=1 << 40):
+    def call(a=None, w=None, bias=FAKE, gelu=0, out=FAKE, dt=1, ldo=40):
         a, w = a or qmat(), w or qmat(block_rows=128)
-        return abi.LIB.rc_qgemm(C.byref(a), C.byref(w), bias, gelu, out, dt, ldo, scratch, nbytes, None)
+        return abi.LIB.rc_qgemm(C.byref(a), C.byref(w), bias, gelu, out, dt, ldo, None)
 
     assert call(a=qmat(block_rows=128)) == -8
     assert call(w=qmat()) == -8
@@ -79,15 +79,9 @@ def test_qgemm_refusals():
     assert call(out=None) == -1
     assert call(out=FAKE + 4) == -3
     assert call(bias=FAKE + 2) == -3
-    assert call(scratch=FAKE + 8) == -3
-    need = abi.rc_qgemm_scratch_bytes(40, 40, 256)
-    if need:
-        assert call(nbytes=need - 1) == -5
-        assert call(scratch=None) == -1
     assert call(a=qmat(rows=1 << 24, scale_ld=1 << 24), w=qmat(block_rows=128, rows=1 << 20, scale_ld=1 << 13),
                 ldo=1 << 20) == -2
     assert call(a=qmat(rows=0)) == 0
-    assert abi.rc_qgemm_scratch_bytes(0, 1, 1) == 0
     if NO_GPU:
         assert call() == -6
 

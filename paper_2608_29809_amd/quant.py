@@ -31,38 +31,50 @@ HEAD_DIM = 72
 BLOCK = 128      # columns (and a weight's rows) that share a scale
 KEY_BLOCK = 64   # tokens of a cache block
 _DTYPES = {torch.float32: abi.RC_F32, torch.bfloat16: abi.RC_BF16}
+_SCALE = 1.0 / math.sqrt(HEAD_DIM)
 
 
-def _need(ok: bool, msg: str):
-    if not ok:
-        raise ValueError(msg)
+_raw_stream = torch._C._cuda_getCurrentRawStream  # (torch.cuda.current_stream takes 2.8 us of a call's 9)
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:
-    _need(t.dtype in _DTYPES, f"{what} is {t.dtype}, not float32 or bfloat16")
-    return _DTYPES[t.dtype]
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        raise ValueError(f"{what} is {t.dtype}, not float32 or bfloat16")
+    return d
 
 
-def _on_gpu(first: torch.Tensor, *others: Optional[torch.Tensor]):
-    _need(first.is_cuda, "the tensors must be on the GPU")
+def _on_gpu(first: torch.Tensor, *others: Optional[torch.Tensor]) -> torch.device:
+    """The one GPU that holds the tensors."""
+    dev = first.device
+    if dev.type != "cuda":
+        raise ValueError(f"the tensors must be on the GPU, not on {dev}")
     for t in others:
-        _need(t is None or t.device == first.device, f"tensors on {first.device} and {t.device if t is not None else None}")
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}")
+    return dev
 
 
 def _call(f, device: torch.device, *args):
     """f(*args, stream) with `device` current and its current stream."""
-    if device.index == torch.cuda.current_device():
-        f(*args, torch.cuda.current_stream().cuda_stream)
+    index = device.index
+    if index == torch.cuda.current_device():
+        f(*args, _raw_stream(index))
     else:
         with torch.cuda.device(device):
-            f(*args, torch.cuda.current_stream().cuda_stream)
+            f(*args, _raw_stream(index))
 
 
-def _rows(t: torch.Tensor, cols: int, what: str):
-    """A [rows][cols] tensor whose rows are contiguous."""
-    _need(t.dim() == 2 and t.shape[1] == cols, f"{what} is {tuple(t.shape)}, not [rows, {cols}]")
-    _need(t.stride(1) == 1 or cols == 1, f"{what}: the values of a row must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0))
+def _ld(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
+    """Elements between the rows of a [rows][cols] tensor whose rows are contiguous."""
+    if t.shape != (rows, cols):
+        raise ValueError(f"{what} is {tuple(t.shape)}, not [{rows}, {cols}]")
+    if t.is_contiguous():
+        return cols
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what}: the values of a row must be contiguous")
+    return ld if rows > 1 else max(cols, ld)
 
 
 class QuantMatrix:
@@ -73,26 +85,35 @@ class QuantMatrix:
     __slots__ = ("data", "scales", "block_rows")
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor, block_rows: int):
-        _need(data.dim() == 2 and data.dtype == torch.float8_e4m3fn, "data must be float8_e4m3fn [rows, cols]")
-        _need(scales.dim() == 2 and scales.dtype == torch.uint8 and scales.stride(1) == 1, "scales must be uint8 rows")
-        _need(block_rows in (1, BLOCK), f"block_rows {block_rows} is not 1 or {BLOCK}")
-        _need(scales.shape[0] == -(-data.shape[1] // BLOCK) and scales.shape[1] >= -(-data.shape[0] // block_rows),
-              f"scales {tuple(scales.shape)} do not cover data {tuple(data.shape)}")
+        if data.dtype != torch.float8_e4m3fn or data.dim() != 2:
+            raise ValueError("data must be float8_e4m3fn [rows, cols]")
+        if scales.dtype != torch.uint8 or scales.dim() != 2 or (scales.stride(1) != 1 and scales.shape[1] > 1):
+            raise ValueError("scales must be uint8 [column blocks, row blocks] with contiguous rows")
+        if block_rows != 1 and block_rows != BLOCK:
+            raise ValueError(f"block_rows {block_rows} is not 1 or {BLOCK}")
+        (rows, cols), (col_blocks, row_blocks) = data.shape, scales.shape
+        if col_blocks != -(-cols // BLOCK) or row_blocks < -(-rows // block_rows) or row_blocks % 16:
+            raise ValueError(f"scales {tuple(scales.shape)} do not cover data {tuple(data.shape)} (row blocks padded to 16)")
         _on_gpu(data, scales)
         self.data, self.scales, self.block_rows = data, scales, block_rows
 
     @classmethod
     def alloc(cls, rows: int, cols: int, block_rows: int = 1, device="cuda") -> "QuantMatrix":
-        data = torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=device)
-        row_blocks = -(-rows // max(block_rows, 1))
-        scales = torch.empty((-(-cols // BLOCK), row_blocks + -row_blocks % 16), dtype=torch.uint8, device=device)
-        return cls(data, scales, block_rows)
+        if block_rows != 1 and block_rows != BLOCK:
+            raise ValueError(f"block_rows {block_rows} is not 1 or {BLOCK}")
+        m = cls.__new__(cls)
+        row_blocks = -(-rows // block_rows)
+        m.data = torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=device)
+        m.scales = torch.empty((-(-cols // BLOCK), row_blocks + -row_blocks % 16), dtype=torch.uint8, device=device)
+        m.block_rows = block_rows
+        return m
 
     def struct(self) -> abi.rc_qmat:
         rows, cols = self.data.shape
-        ld = _rows(self.data, cols, "data")
-        scale_ld = self.scales.stride(0) if self.scales.shape[0] > 1 else self.scales.shape[1]
-        return abi.rc_qmat(self.data.data_ptr(), self.scales.data_ptr(), ld, rows, cols, scale_ld, self.block_rows)
+        col_blocks, row_blocks = self.scales.shape
+        scale_ld = row_blocks if col_blocks == 1 else self.scales.stride(0)
+        return abi.rc_qmat(self.data.data_ptr(), self.scales.data_ptr(), _ld(self.data, rows, cols, "data"), rows, cols,
+                           scale_ld, self.block_rows)
 
 
 class QuantCache:
@@ -104,19 +125,25 @@ class QuantCache:
     __slots__ = ("data", "scales", "batch", "heads", "tokens")
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor):
-        _need(data.dim() == 6 and tuple(data.shape[3:]) == (2, KEY_BLOCK, HEAD_DIM) and data.dtype == torch.float8_e4m3fn,
-              f"data must be float8_e4m3fn [batch, heads, blocks, 2, {KEY_BLOCK}, {HEAD_DIM}]")
-        _need(scales.dtype == torch.uint8 and scales.shape == data.shape[:4], "scales must be uint8 [batch, heads, blocks, 2]")
-        _need(data.numel() > 0, "the cache is empty")
-        _need(data[0].is_contiguous() and scales[0].is_contiguous(), "a chain of the cache must be contiguous")
+        shape = data.shape
+        if data.dtype != torch.float8_e4m3fn or len(shape) != 6 or shape[3:] != (2, KEY_BLOCK, HEAD_DIM):
+            raise ValueError(f"data must be float8_e4m3fn [batch, heads, blocks, 2, {KEY_BLOCK}, {HEAD_DIM}]")
+        if scales.dtype != torch.uint8 or scales.shape != shape[:4]:
+            raise ValueError("scales must be uint8 [batch, heads, blocks, 2]")
+        batch, heads, blocks = shape[:3]
+        if not (batch and heads and blocks):
+            raise ValueError("the cache is empty")
+        if not (data.is_contiguous() or data[0].is_contiguous()) or not (scales.is_contiguous() or scales[0].is_contiguous()):
+            raise ValueError("a chain of the cache must be contiguous")
         _on_gpu(data, scales)
         self.data, self.scales = data, scales
-        self.batch, self.heads, self.tokens = data.shape[0], data.shape[1], data.shape[2] * KEY_BLOCK
+        self.batch, self.heads, self.tokens = batch, heads, blocks * KEY_BLOCK
 
     @classmethod
     def alloc(cls, batch: int, heads: int, tokens: int, device="cuda") -> "QuantCache":
         """A cache of zeros."""
-        _need(tokens > 0 and tokens % KEY_BLOCK == 0, f"tokens {tokens} is not a positive multiple of {KEY_BLOCK}")
+        if tokens <= 0 or tokens % KEY_BLOCK:
+            raise ValueError(f"tokens {tokens} is not a positive multiple of {KEY_BLOCK}")
         shape = (batch, heads, tokens // KEY_BLOCK, 2)
         return cls(torch.zeros(shape + (KEY_BLOCK, HEAD_DIM), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn),
                    torch.zeros(shape, dtype=torch.uint8, device=device))
@@ -131,14 +158,19 @@ def quantize(x: torch.Tensor, block_rows: int = 1, out: Optional[QuantMatrix] = 
     with a scale for each row and 128 columns (block_rows 1) or each 128 x 128
     tile (128)."""
     dtype = _dtype(x, "x")
-    _need(x.dim() == 2, f"x is {tuple(x.shape)}, not [rows, cols]")
-    ldx = _rows(x, x.shape[1], "x")
+    if x.dim() != 2:
+        raise ValueError(f"x is {tuple(x.shape)}, not [rows, cols]")
+    rows, cols = x.shape
+    ldx = _ld(x, rows, cols, "x")
     if out is None:
-        out = QuantMatrix.alloc(x.shape[0], x.shape[1], block_rows, x.device)
-    _need(out.data.shape == x.shape and out.block_rows == block_rows, "out has another shape or other blocks")
-    _on_gpu(x, out.data)
-    if x.shape[0]:
-        _call(abi.rc_quantize, x.device, x.data_ptr(), dtype, ldx, C.byref(out.struct()))
+        dev = _on_gpu(x)
+        out = QuantMatrix.alloc(rows, cols, block_rows, dev)
+    else:
+        dev = _on_gpu(x, out.data)
+        if out.data.shape != x.shape or out.block_rows != block_rows:
+            raise ValueError("out has another shape or other blocks")
+    if rows:
+        _call(abi.rc_quantize, dev, x.data_ptr(), dtype, ldx, C.byref(out.struct()))
     return out
 
 
@@ -147,16 +179,16 @@ def qgemm(a: QuantMatrix, w: QuantMatrix, bias: Optional[torch.Tensor] = None, g
     """act(a w^T + bias): a [m, k] with block_rows 1, w [n, k] with block_rows
     128, bias float32 [n]; the result [m, n] in dtype (or in out)."""
     m, n = a.data.shape[0], w.data.shape[0]
-    _need(bias is None or (bias.dtype == torch.float32 and tuple(bias.shape) == (n,) and bias.is_contiguous()),
-          f"bias must be contiguous float32 [{n}]")
+    if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,) or not bias.is_contiguous()):
+        raise ValueError(f"bias must be contiguous float32 [{n}]")
     if out is None:
-        _need(dtype in _DTYPES, f"dtype {dtype} is not float32 or bfloat16")
+        if dtype not in _DTYPES:
+            raise ValueError(f"dtype {dtype} is not float32 or bfloat16")
         out = torch.empty((m, n), dtype=dtype, device=a.data.device)
-    _need(out.shape == (m, n), f"out is {tuple(out.shape)}, not [{m}, {n}]")
-    ldo = _rows(out, n, "out")
-    _on_gpu(a.data, w.data, bias, out)
+    ldo = _ld(out, m, n, "out")
+    dev = _on_gpu(a.data, w.data, bias, out)
     if m:
-        _call(abi.rc_qgemm, out.device, C.byref(a.struct()), C.byref(w.struct()), None if bias is None else bias.data_ptr(),
+        _call(abi.rc_qgemm, dev, C.byref(a.struct()), C.byref(w.struct()), None if bias is None else bias.data_ptr(),
               1 if gelu else 0, out.data_ptr(), _dtype(out, "out"), ldo)
     return out
 
@@ -165,14 +197,13 @@ def qcache_store(cache: QuantCache, active: ActiveSet, k: torch.Tensor, v: torch
     """Merge the fresh keys and values of the active tokens into the cache:
     k, v [active tokens, heads * 72] float32 or bfloat16 with one row stride
     (views of one product's output will do)."""
-    dtype, cols = _dtype(k, "k"), cache.heads * HEAD_DIM
-    ld = _rows(k, cols, "k")
-    _need(v.dtype == k.dtype and v.shape == k.shape and _rows(v, cols, "v") == ld, "k and v must be alike")
-    _need(k.shape[0] == active.total, f"{k.shape[0]} rows for {active.total} active tokens")
-    _on_gpu(cache.data, k, v, active.idx, active.offsets)
-    if active.total:
-        _call(abi.rc_qcache_store, cache.data.device, C.byref(cache.struct()), C.byref(active.struct()), k.data_ptr(),
-              v.data_ptr(), dtype, ld)
+    dtype, cols, rows = _dtype(k, "k"), cache.heads * HEAD_DIM, active.total
+    ld = _ld(k, rows, cols, "k")
+    if v.dtype != k.dtype or _ld(v, rows, cols, "v") != ld:
+        raise ValueError("k and v must have one type and row stride")
+    dev = _on_gpu(cache.data, k, v, active.idx, active.offsets)
+    if rows:
+        _call(abi.rc_qcache_store, dev, C.byref(cache.struct()), C.byref(active.struct()), k.data_ptr(), v.data_ptr(), dtype, ld)
 
 
 def qcache_attention(cache: QuantCache, rows: ActiveSet, q: torch.Tensor, scale: Optional[float] = None,
@@ -181,22 +212,23 @@ def qcache_attention(cache: QuantCache, rows: ActiveSet, q: torch.Tensor, scale:
     read) over the first key_len[b] keys (default: all) of their chain.
     q [rows, heads * 72] bfloat16; scale defaults to 1/sqrt(72); key_len int32
     [batch] on the GPU; rows of a chain without keys are 0."""
-    cols = cache.heads * HEAD_DIM
-    _need(q.dtype == torch.bfloat16, f"q is {q.dtype}, not bfloat16")
-    ldq = _rows(q, cols, "q")
-    _need(q.shape[0] == rows.total, f"{q.shape[0]} rows for {rows.total} in the set")
-    _need(key_len is None or (key_len.dtype == torch.int32 and tuple(key_len.shape) == (cache.batch,) and
-                              key_len.is_contiguous()), f"key_len must be contiguous int32 [{cache.batch}]")
+    cols, total = cache.heads * HEAD_DIM, rows.total
+    if q.dtype != torch.bfloat16:
+        raise ValueError(f"q is {q.dtype}, not bfloat16")
+    ldq = _ld(q, total, cols, "q")
+    if key_len is not None and (key_len.dtype != torch.int32 or key_len.shape != (cache.batch,) or not key_len.is_contiguous()):
+        raise ValueError(f"key_len must be contiguous int32 [{cache.batch}]")
     if out is None:
-        out = torch.empty((q.shape[0], cols), dtype=torch.bfloat16, device=q.device)
-    _need(out.dtype == torch.bfloat16 and out.shape == q.shape, f"out must be bfloat16 {tuple(q.shape)}")
-    ldo = _rows(out, cols, "out")
-    _on_gpu(cache.data, q, out, key_len, rows.offsets)
-    if rows.total:
+        out = torch.empty((total, cols), dtype=torch.bfloat16, device=q.device)
+    elif out.dtype != torch.bfloat16:
+        raise ValueError(f"out is {out.dtype}, not bfloat16")
+    ldo = _ld(out, total, cols, "out")
+    dev = _on_gpu(cache.data, q, out, key_len, rows.offsets)
+    if total:
         c, s = cache.struct(), rows.struct()
         nbytes = abi.rc_qcache_attention_scratch_bytes(C.byref(c), C.byref(s))
-        scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
-        _call(abi.rc_qcache_attention, q.device, C.byref(c), C.byref(s), None if key_len is None else key_len.data_ptr(),
-              q.data_ptr(), ldq, 1.0 / math.sqrt(HEAD_DIM) if scale is None else float(scale), out.data_ptr(), ldo,
+        scratch = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+        _call(abi.rc_qcache_attention, dev, C.byref(c), C.byref(s), None if key_len is None else key_len.data_ptr(),
+              q.data_ptr(), ldq, _SCALE if scale is None else float(scale), out.data_ptr(), ldo,
               scratch.data_ptr() if nbytes else None, nbytes)
     return out

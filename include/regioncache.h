@@ -440,6 +440,44 @@ rc_status rc_qcache_attention(const rc_qcache *cache, const rc_active_set *rows,
                               const void *q, int64_t ldq, float scale, void *out, int64_t ldo, void *scratch,
                               size_t scratch_bytes, void *stream);
 
+/* STEPS ON AN 8-BIT POOL.  The pool may hold the keys and values of every slot
+ * in 8 bits, as an rc_qcache of that slot (hidden states stay bfloat16: two
+ * thirds of the bytes, and half of those that attention reads).  bf16 storage
+ * only (RC_ERR_UNSUPPORTED otherwise).  A slot holds the keys and values
+ * [heads][N/64][2][64][72], their scale bytes [heads][N/64][2] and H [N][C];
+ * latents as in the ordinary pool.  rc_quant_cache_offsets gives the byte
+ * offsets of the three parts; consecutive chains' slots are
+ * steps*layers slots apart.  A pool that region steps read must have been
+ * filled by dense steps, or start as zeroed memory. */
+size_t rc_quant_cache_bytes(const rc_ctx *ctx, int32_t batch, int32_t steps);
+rc_status rc_quant_cache_offsets(const rc_ctx *ctx, const rc_cache_view *cache, int32_t b, int32_t t, int32_t l,
+                                 size_t *data_off, size_t *scales_off, size_t *h_off);
+rc_status rc_quant_cache_latent_offset(const rc_ctx *ctx, const rc_cache_view *cache, int32_t b, int32_t t,
+                                       size_t *off);
+/* Workspace of the two steps below (takes the place of rc_workspace_bytes). */
+size_t rc_quant_workspace_bytes(const rc_ctx *ctx, int32_t max_rows, int32_t batch);
+
+/* One block's weights of the steps below in 8 bits (block_rows 128): QKV
+ * [3C][C] and the MLP's two, [F][C] and [C][F].  rc_set_quant_weights copies the
+ * HOST array of config.layers entries (device pointers stay the caller's) and
+ * makes the following steps on an 8-bit pool take these three products from
+ * them, with activations quantised row by row; NULL returns to the bfloat16
+ * weights.  Steps on other pools are not affected. */
+typedef struct {
+  rc_qmat qkv_w, fc1_w, fc2_w;
+} rc_quant_layer;
+rc_status rc_set_quant_weights(rc_ctx *ctx, const rc_quant_layer *layers);
+
+/* rc_build_cache and rc_reuse_step (RC_FUSE_UPDATE required, RC_VALIDATE
+ * allowed) on an 8-bit pool, at most 2^24 rows in a call: the fresh keys and
+ * values are merged into the slot as by rc_qcache_store, and the queries attend
+ * over it as by rc_qcache_attention. */
+rc_status rc_build_cache_quant(rc_ctx *ctx, const rc_cache_view *cache, int32_t step, const rc_step_io *io,
+                               void *workspace, size_t workspace_bytes, void *stream);
+rc_status rc_reuse_step_quant(rc_ctx *ctx, const rc_cache_view *cache, int32_t step,
+                              const rc_active_set *active, const rc_step_io *io, uint32_t flags,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
 /* Wait for `stream`; returns RC_ERR_HIP if any enqueued work failed. */
 rc_status rc_sync(void *stream);
 

@@ -86,6 +86,10 @@ class rc_qcache(C.Structure):
                 ("scale_stride", C.c_int64), ("batch", C.c_int32), ("heads", C.c_int32), ("tokens", C.c_int32)]
 
 
+class rc_quant_layer(C.Structure):
+    _fields_ = [("qkv_w", rc_qmat), ("fc1_w", rc_qmat), ("fc2_w", rc_qmat)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with paper_2608_29809_amd/build.py "
@@ -125,6 +129,14 @@ def _load():
         "rc_qcache_store": (C.c_int, [QC, AS, P, P, I32, I64, P]),
         "rc_qcache_attention_scratch_bytes": (S, [QC, AS]),
         "rc_qcache_attention": (C.c_int, [QC, AS, P, P, I64, C.c_float, P, I64, P, S, P]),
+        "rc_quant_cache_bytes": (S, [P, I32, I32]),
+        "rc_quant_workspace_bytes": (S, [P, I32, I32]),
+        "rc_quant_cache_offsets": (C.c_int, [P, C.POINTER(rc_cache_view), I32, I32, I32, C.POINTER(S), C.POINTER(S),
+                                             C.POINTER(S)]),
+        "rc_quant_cache_latent_offset": (C.c_int, [P, C.POINTER(rc_cache_view), I32, I32, C.POINTER(S)]),
+        "rc_set_quant_weights": (C.c_int, [P, C.POINTER(rc_quant_layer)]),
+        "rc_build_cache_quant": (C.c_int, [P, C.POINTER(rc_cache_view), I32, C.POINTER(rc_step_io), P, S, P]),
+        "rc_reuse_step_quant": (C.c_int, [P, C.POINTER(rc_cache_view), I32, AS, C.POINTER(rc_step_io), U32, P, S, P]),
         "rc_sync": (C.c_int, [P]),
         "rc_set_kernel_timing": (C.c_int, [P, I32]),
         "rc_get_kernel_timing": (C.c_int, [P, I32, C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
@@ -163,7 +175,9 @@ def _wrap(name):
 for _n in ["rc_create", "rc_cache_offsets", "rc_cache_latent_offset", "rc_prepare_text", "rc_build_cache",
            "rc_reuse_step", "rc_update_cache", "rc_validate_active", "rc_reuse_step_hosted", "rc_build_cache_hosted",
            "rc_localize_region", "rc_maps_from_logits", "rc_maps_from_logits_noalloc", "rc_compact_mask", "rc_sync", "rc_set_kernel_timing",
-           "rc_get_kernel_timing", "rc_quantize", "rc_qgemm", "rc_qcache_store", "rc_qcache_attention"]:
+           "rc_get_kernel_timing", "rc_quantize", "rc_qgemm", "rc_qcache_store", "rc_qcache_attention",
+           "rc_quant_cache_offsets", "rc_quant_cache_latent_offset", "rc_set_quant_weights", "rc_build_cache_quant",
+           "rc_reuse_step_quant"]:
     globals()[_n] = _wrap(_n)
 
 rc_destroy = LIB.rc_destroy
@@ -173,3 +187,5 @@ rc_workspace_bytes = LIB.rc_workspace_bytes
 rc_staging_bytes = LIB.rc_staging_bytes
 rc_maps_from_logits_scratch_bytes = LIB.rc_maps_from_logits_scratch_bytes
 rc_qcache_attention_scratch_bytes = LIB.rc_qcache_attention_scratch_bytes
+rc_quant_cache_bytes = LIB.rc_quant_cache_bytes
+rc_quant_workspace_bytes = LIB.rc_quant_workspace_bytes

@@ -75,6 +75,7 @@ struct rc_ctx {
   rc_model_config cfg;
   rc_weights w;
   std::vector<rc_layer_weights> layers;
+  std::vector<rc_quant_layer> quant;  // 8-bit weights of the steps on an 8-bit pool, or empty
   int N, C, H, F, L, M, Mp;
   size_t esz;
   bool vec16;  // every bias and modulation table is 16-byte aligned (not checked by rc_create)
@@ -161,6 +162,44 @@ WsLayout ws_layout(const rc_ctx *c, int max_rows, int B) {
   return w;
 }
 
+// 8-bit pool: a slot holds the keys and values [heads][N/64][2][64][72] e4m3,
+// their scale bytes [heads][N/64][2], and H [N][C] in bfloat16.
+size_t quant_scales_off(const rc_ctx *c) { return (size_t)2 * c->N * c->C; }
+size_t quant_h_off(const rc_ctx *c) { return quant_scales_off(c) + align256((size_t)c->H * (c->N / 64) * 2); }
+size_t quant_slot_bytes(const rc_ctx *c) { return quant_h_off(c) + align256((size_t)c->N * c->C * 2); }
+size_t quant_slot_offset(const rc_ctx *c, int T, int b, int t, int l) {
+  return (((size_t)b * T + t) * c->L + l) * quant_slot_bytes(c);
+}
+size_t quant_latent_offset(const rc_ctx *c, int B, int T, int b, int t) {
+  return (size_t)B * T * c->L * quant_slot_bytes(c) + ((size_t)b * (T + 1) + t) * latent_floats(c) * sizeof(float);
+}
+size_t quant_cache_bytes(const rc_ctx *c, int B, int T) {
+  return quant_latent_offset(c, B, T, 0, 0) + (c->cfg.token_mode ? 0 : (size_t)B * (T + 1) * latent_floats(c) * sizeof(float));
+}
+
+// What a step on an 8-bit pool needs behind the workspace of an ordinary one.
+struct QuantWs {
+  size_t qkv, a, as, g, gs, y, part, total;
+  int scale_ld;
+};
+QuantWs quant_ws(const rc_ctx *c, int max_rows) {
+  QuantWs w{};
+  size_t o = 0;
+  auto take = [&](size_t bytes) { size_t at = o; o = align256(o + bytes); return at; };
+  const size_t R = (size_t)std::max(max_rows, 1);
+  w.scale_ld = (int)((R + 15) & ~size_t(15));
+  w.qkv = take(R * 3 * c->C * 2);
+  w.a = take(R * c->C);
+  w.as = take((size_t)(c->C / rc::kQBlock) * w.scale_ld);
+  w.g = take(R * c->F);
+  w.gs = take((size_t)(c->F / rc::kQBlock) * w.scale_ld);
+  w.y = take(R * c->C * sizeof(float));
+  const size_t split = std::min(R * c->H * rc::kQMaxSplits, (size_t)rc::kQMaxSplitRows);
+  w.part = take(split * (rc::kHeadDim + 2) * sizeof(float) + 256);
+  w.total = o;
+  return w;
+}
+
 // ------------------------------------------------------------------ timing
 
 template <typename F> rc_status timed(rc_ctx *c, int cls, hipStream_t s, F &&launch) {
@@ -199,14 +238,14 @@ template <typename F> rc_status timed(rc_ctx *c, int cls, hipStream_t s, F &&lau
 
 // ------------------------------------------------------------------ validation helpers
 
-rc_status check_cache(const rc_ctx *c, const rc_cache_view *cache, int step) {
+rc_status check_cache(const rc_ctx *c, const rc_cache_view *cache, int step, bool quant = false) {
   RC_CHECK(cache, RC_ERR_INVALID_ARG, "cache is null");
   RC_CHECK(cache->base, RC_ERR_INVALID_ARG, "cache->base is null");
   RC_CHECK(aligned16(cache->base), RC_ERR_ALIGN, "cache->base not 16-byte aligned");
   RC_CHECK(cache->batch >= 1 && cache->batch <= 32767, RC_ERR_SHAPE, "cache->batch %d out of range", cache->batch);
   RC_CHECK(cache->steps >= 1, RC_ERR_SHAPE, "cache->steps %d < 1", cache->steps);
   RC_CHECK(step >= 0 && step < cache->steps, RC_ERR_SHAPE, "step %d outside [0, %d)", step, cache->steps);
-  const size_t need = cache_bytes(c, cache->batch, cache->steps);
+  const size_t need = quant ? quant_cache_bytes(c, cache->batch, cache->steps) : cache_bytes(c, cache->batch, cache->steps);
   RC_CHECK(cache->bytes >= need, RC_ERR_CAPACITY, "cache has %zu bytes, needs %zu", cache->bytes, need);
   return RC_OK;
 }
@@ -345,7 +384,7 @@ struct PipeJoin {
 template <typename T>
 rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_step_io *io, bool dense,
                    const rc_active_set *act, void *active_hidden, bool fuse, void *ws, size_t ws_bytes,
-                   hipStream_t s, const HostPipe *hp = nullptr) {
+                   hipStream_t s, const HostPipe *hp = nullptr, bool quant = false) {
   const int B = cache->batch, N = c->N, C = c->C, H = c->H, F = c->F, L = c->L, T_ = cache->steps;
   std::vector<int> counts(B);
   int R = 0, max_rb = 0;
@@ -363,8 +402,9 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
   const WsLayout wl = ws_layout(c, R, B);
   RC_CHECK(ws, RC_ERR_INVALID_ARG, "workspace is null");
   RC_CHECK(aligned16(ws), RC_ERR_ALIGN, "workspace not 16-byte aligned");
-  RC_CHECK(ws_bytes >= wl.total, RC_ERR_CAPACITY, "workspace has %zu bytes, needs %zu for %d rows", ws_bytes,
-           wl.total, R);
+  const QuantWs qw = quant ? quant_ws(c, R) : QuantWs{};
+  RC_CHECK(ws_bytes >= wl.total + qw.total, RC_ERR_CAPACITY, "workspace has %zu bytes, needs %zu for %d rows", ws_bytes,
+           wl.total + qw.total, R);
   if (!dense && !fuse && R > 0) {
     RC_CHECK(active_hidden, RC_ERR_INVALID_ARG, "active_hidden is null without RC_FUSE_UPDATE");
     RC_CHECK(aligned16(active_hidden), RC_ERR_ALIGN, "active_hidden not 16-byte aligned");
@@ -374,8 +414,9 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
   char *cb = (char *)cache->base;
   const size_t n_lat = c->cfg.token_mode ? 0 : latent_floats(c);
   const long long lat_chain_stride = (long long)(T_ + 1) * n_lat;
-  float *traj_t = c->cfg.token_mode ? nullptr : (float *)(cb + latent_offset(c, B, T_, 0, step));
-  float *traj_next = c->cfg.token_mode ? nullptr : (float *)(cb + latent_offset(c, B, T_, 0, step + 1));
+  auto lat_off = [&](int t) { return quant ? quant_latent_offset(c, B, T_, 0, t) : latent_offset(c, B, T_, 0, t); };
+  float *traj_t = c->cfg.token_mode ? nullptr : (float *)(cb + lat_off(step));
+  float *traj_next = c->cfg.token_mode ? nullptr : (float *)(cb + lat_off(step + 1));
 
   if (R == 0) {  // nothing active: slot untouched, latent from the cached trajectory
     if (!c->cfg.token_mode)
@@ -415,7 +456,8 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
   // step for all blocks.
   int fold_nt = 0;
   bool fold_uv = false;
-  if (sizeof(T) == 2) {
+  const bool q_mm = quant && !c->quant.empty();  // QKV and MLP products from 8-bit weights
+  if (sizeof(T) == 2 && !q_mm) {
     const rc::GemmPlan px = plan(c, R, C, C, gpf, rc::EPI_RESID), p1 = plan(c, R, F, C, gpf, rc::EPI_GELU);
     const int tile = px.big ? 144 : px.bn;  // producer's statistics tiles
     if (px.splits == 1 && p1.splits == 1 && C % tile == 0 && C / tile <= rc::kFoldMaxTiles) fold_nt = C / tile;
@@ -500,9 +542,40 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
   const bool emit = io->maps && io->n_delta > 0;
   // device pool: slot (b, step, l) in place; host-resident pool: entry
   // l % kRing of the staging ring, chains one slot apart
-  const long long slot_chain_stride = hp ? (long long)slot_elems(c) : (long long)T_ * L * slot_elems(c);
+  const long long slot_chain_stride = hp      ? (long long)slot_elems(c)
+                                      : quant ? (long long)T_ * L * (quant_slot_bytes(c) / 2)
+                                              : (long long)T_ * L * slot_elems(c);
   const size_t kv_half = (size_t)H * N * rc::kHeadDim;
   const float scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)rc::kHeadDim));
+
+  // 8-bit pool: the layer's products and attention
+  char *qws = wsb + wl.total;
+  uint8_t *qa = (uint8_t *)(qws + qw.a), *qas = (uint8_t *)(qws + qw.as);
+  auto norm_quant = [&](int cls, int l, int shift_row, const rc::NormQuantArgs &with) -> rc_status {
+    rc::NormQuantArgs a = with;
+    a.X = X; a.rows = R; a.C = C; a.eps = c->cfg.ln_eps; a.t0 = t0; a.shift_row = shift_row;
+    a.sst = c->layers[std::min(l, L - 1)].sst;
+    if (l < L) { a.q = qa; a.scales = qas; a.scale_ld = qw.scale_ld; }
+    return timed(c, cls, s, [&] { return rc::launch_norm_quantize(a, s); });
+  };
+  auto qgemm = [&](int cls, const uint8_t *a, const uint8_t *as, const rc_qmat &w, const float *bias, bool gelu, bool f32,
+                   void *out) -> rc_status {
+    rc::QGemmArgs g{};
+    g.a = a; g.as = as; g.lda = w.cols; g.as_ld = qw.scale_ld;
+    g.w = (const uint8_t *)w.data; g.ws = w.scales; g.ldw = w.ld; g.ws_ld = w.scale_ld;
+    g.M = R; g.N = w.rows; g.K = w.cols; g.bias = bias; g.out = out; g.ldo = w.rows;
+    return timed(c, cls, s, [&] { return rc::launch_qgemm(g, rc::plan_qgemm(g.M, g.N, g.K), gelu, f32, s); });
+  };
+  rc::ChainRows q_rows{};
+  rc::QAttnPlan q_plan{1, 1};
+  if (quant) {
+    std::vector<int> offs(B + 1);
+    for (int b = 0; b <= B; ++b) offs[b] = dense ? b * N : act->offsets_host[b];
+    q_rows.offsets = offsets_dev;
+    q_rows.n_arg = std::min(B, rc::kQArgChains);
+    for (int b = 0; b <= q_rows.n_arg; ++b) q_rows.arg[b] = offs[b];
+    q_plan = rc::plan_qattention(offs.data(), B, H, N);
+  }
 
   PipeJoin pipe_join{c, s};
   auto upload = [&](int l) -> rc_status {  // keys and values of block l, every chain, on the copy stream
@@ -538,18 +611,48 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
   bool a1_ready = false;  // the previous block's MLP reduction already wrote this block's LN1 rows
   for (int l = 0; l < L; ++l) {
     const rc_layer_weights &lw = c->layers[l];
-    T *slot = hp ? (T *)(hp->staging + (size_t)(l % kRing) * hp->entry_bytes)
-                 : (T *)(cb + slot_offset(c, T_, 0, step, l));
-    T *Ks = slot, *Vs = slot + kv_half, *Hs = slot + 2 * kv_half;
+    char *qslot = quant ? cb + quant_slot_offset(c, T_, 0, step, l) : nullptr;
+    T *slot = hp      ? (T *)(hp->staging + (size_t)(l % kRing) * hp->entry_bytes)
+              : quant ? nullptr
+                      : (T *)(cb + slot_offset(c, T_, 0, step, l));
+    T *Ks = slot, *Vs = quant ? nullptr : slot + kv_half, *Hs = quant ? (T *)(qslot + quant_h_off(c)) : slot + 2 * kv_half;
     if (hp) {
       if (!dense) RC_HIP(hipStreamWaitEvent(s, c->up_ev[l % kRing], 0));  // this block's keys/values are in
       else if (l >= kRing) RC_HIP(hipStreamWaitEvent(s, c->wb_ev[l % kRing], 0));  // the entry was written back
     }
 
-    if (!a1_ready)
-      RC_TRY(timed(c, RC_KC_NORM, s, [&] { return rc::launch_ln_mod<T>(X, R, C, lw.sst, t0, 0, c->cfg.ln_eps, A1, s); }));
+    if (!a1_ready) {
+      if (q_mm) RC_TRY(norm_quant(RC_KC_NORM, l, 0, rc::NormQuantArgs{}));
+      else RC_TRY(timed(c, RC_KC_NORM, s, [&] { return rc::launch_ln_mod<T>(X, R, C, lw.sst, t0, 0, c->cfg.ln_eps, A1, s); }));
+    }
     a1_ready = false;
-    {  // QKV with the K/V scatter into the slot
+    if (quant) {  // QKV rows, keys and values merged into the 8-bit slot, attention over the whole slot
+      bf16 *qkv = (bf16 *)(qws + qw.qkv);  // [R][3C]
+      if (q_mm) {
+        RC_TRY(qgemm(RC_KC_GEMM_QKV, qa, qas, c->quant[l].qkv_w, lw.qkv_b, false, false, qkv));
+      } else {
+        rc::GemmArgs g{};
+        g.A = A1; g.W = lw.qkv_w; g.bias = lw.qkv_b; g.M = R; g.N = 3 * C; g.K = C; g.lda = C; g.out = qkv; g.ldo = 3 * C;
+        g.warm = lw.proj_w; g.warm_lines = wlines(C, C);
+        RC_TRY(gemm<T>(c, RC_KC_GEMM_QKV, g, rc::EPI_STORE, gpart, gpf, s));
+      }
+      rc::QCacheArgs qc{};
+      qc.data = (uint8_t *)qslot; qc.scales = (uint8_t *)qslot + quant_scales_off(c);
+      qc.chain_stride = qc.scale_chain_stride = (long long)T_ * L * quant_slot_bytes(c);
+      qc.heads = H; qc.tokens = N;
+      rc::QStoreArgs sa{};
+      sa.c = qc; sa.rows = q_rows; sa.idx = dense ? nullptr : act->idx; sa.k = qkv + C; sa.v = qkv + 2 * C; sa.ld = 3 * C;
+      RC_TRY(timed(c, RC_KC_MISC, s, [&] { return rc::launch_qcache_store<bf16>(sa, B, s); }));
+      rc::QAttnArgs a{};
+      a.c = qc; a.rows = q_rows; a.q = qkv; a.ldq = 3 * C; a.scale_log2 = scale_log2; a.out = (bf16 *)O; a.ldo = C;
+      a.splits = q_plan.splits; a.total_rows = R;
+      a.part = (float *)(qws + qw.part);
+      a.ml = a.part + (q_plan.splits > 1 ? (size_t)q_plan.splits * R * C : 0);
+      RC_TRY(timed(c, RC_KC_ATTN_SELF, s, [&] { return rc::launch_qattention(a, B, max_rb, q_plan.qh, s); }));
+      if (a.splits > 1)
+        RC_TRY(timed(c, RC_KC_ATTN_COMBINE, s, [&] { return rc::launch_qattention_combine(a, s); }));
+    }
+    if (!quant) {  // QKV with the K/V scatter into the slot
       rc::GemmArgs g{};
       g.A = A1; g.W = lw.qkv_w; g.bias = lw.qkv_b; g.M = R; g.N = 3 * C; g.K = C; g.lda = C;
       g.out = Q; g.ldo = C; g.rows = rows; g.kslot = Ks; g.vslot = Vs;
@@ -558,7 +661,7 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
       g.warm = lw.proj_w; g.warm_lines = wlines(C, C);
       RC_TRY(gemm<T>(c, RC_KC_GEMM_QKV, g, rc::EPI_QKV, gpart, gpf, s));
     }
-    {  // region-level sparse self-attention over the whole slot
+    if (!quant) {  // region-level sparse self-attention over the whole slot
       rc::AttnArgs a{};
       a.Q = Q; a.K = Ks; a.V = Vs; a.v_rowmajor = 1; a.chain_stride = slot_chain_stride; a.head_stride = (long long)N * rc::kHeadDim;
       set_offsets(a); a.n_keys = N; a.n_valid = N; a.hidden = C; a.splits = splits;
@@ -627,6 +730,22 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
       if (!dense) { g.warm = (const char *)lw.fc2_w + fc2_half * 128; g.warm_lines = fc2_lines - fc2_half; }
       else { g.warm = lw.fc2_w; g.warm_lines = fc2_lines; }
       RC_TRY(gemm<T>(c, RC_KC_GEMM_XPROJ, g, rc::EPI_RESID, gpart, gpf, s));
+    }
+    if (q_mm) {  // MLP from 8-bit weights; merge into the cached hidden state and the next block's LayerNorm in one pass
+      uint8_t *qg = (uint8_t *)(qws + qw.g), *qgs = (uint8_t *)(qws + qw.gs);
+      float *y = (float *)(qws + qw.y);
+      RC_TRY(norm_quant(RC_KC_NORM, l, 3, rc::NormQuantArgs{}));
+      RC_TRY(qgemm(RC_KC_GEMM_FC1, qa, qas, c->quant[l].fc1_w, lw.fc1_b, true, false, G));
+      rc::QuantArgs ga{};
+      ga.x = G; ga.ldx = F; ga.rows = R; ga.cols = F; ga.q = qg; ga.ldq = F; ga.scales = qgs; ga.scale_ld = qw.scale_ld;
+      RC_TRY(timed(c, RC_KC_MISC, s, [&] { return rc::launch_quantize<bf16>(ga, 1, s); }));
+      RC_TRY(qgemm(RC_KC_GEMM_FC2, qg, qgs, c->quant[l].fc2_w, nullptr, false, true, y));
+      rc::NormQuantArgs na{};
+      na.y = y; na.bias = lw.fc2_b; na.gate = lw.sst + 5 * C; na.gate2 = t0 + 5 * C; na.packed = rows;
+      na.hslot = (bf16 *)Hs; na.chain_stride = slot_chain_stride;
+      RC_TRY(norm_quant(RC_KC_SPLIT_FINISH, l + 1, 0, na));
+      a1_ready = true;
+      continue;
     }
     if (!fold_nt)
       RC_TRY(timed(c, RC_KC_NORM, s, [&] { return rc::launch_ln_mod<T>(X, R, C, lw.sst, t0, 3, c->cfg.ln_eps, A1, s); }));
@@ -1206,6 +1325,97 @@ rc_status rc_build_cache_hosted(rc_ctx *c, const rc_cache_view *cache, int32_t s
   return run_step<bf16>(c, &dev, step, io, true, nullptr, nullptr, true, ws, ws_bytes, (hipStream_t)stream, &hp);
 }
 
+size_t rc_quant_cache_bytes(const rc_ctx *c, int32_t batch, int32_t steps) {
+  if (!c || c->esz != 2 || batch < 1 || steps < 1) return 0;
+  return quant_cache_bytes(c, batch, steps);
+}
+
+size_t rc_quant_workspace_bytes(const rc_ctx *c, int32_t max_rows, int32_t batch) {
+  if (!c || c->esz != 2 || batch < 1 || max_rows < 0) return 0;
+  return ws_layout(c, max_rows, batch).total + quant_ws(c, max_rows).total;
+}
+
+rc_status rc_quant_cache_offsets(const rc_ctx *c, const rc_cache_view *cache, int32_t b, int32_t t, int32_t l,
+                                 size_t *data_off, size_t *scales_off, size_t *h_off) {
+  RC_CHECK(c && cache, RC_ERR_INVALID_ARG, "null argument");
+  RC_CHECK(c->esz == 2, RC_ERR_UNSUPPORTED, "the 8-bit pool needs bf16 storage");
+  RC_CHECK(b >= 0 && b < cache->batch && t >= 0 && t < cache->steps && l >= 0 && l < c->L, RC_ERR_SHAPE,
+           "slot (%d, %d, %d) out of range", b, t, l);
+  const size_t base = quant_slot_offset(c, cache->steps, b, t, l);
+  if (data_off) *data_off = base;
+  if (scales_off) *scales_off = base + quant_scales_off(c);
+  if (h_off) *h_off = base + quant_h_off(c);
+  return RC_OK;
+}
+
+rc_status rc_quant_cache_latent_offset(const rc_ctx *c, const rc_cache_view *cache, int32_t b, int32_t t, size_t *off) {
+  RC_CHECK(c && cache && off, RC_ERR_INVALID_ARG, "null argument");
+  RC_CHECK(c->esz == 2, RC_ERR_UNSUPPORTED, "the 8-bit pool needs bf16 storage");
+  RC_CHECK(!c->cfg.token_mode, RC_ERR_SHAPE, "token mode keeps no latent trajectory");
+  RC_CHECK(b >= 0 && b < cache->batch && t >= 0 && t <= cache->steps, RC_ERR_SHAPE, "latent (%d, %d) out of range",
+           b, t);
+  *off = quant_latent_offset(c, cache->batch, cache->steps, b, t);
+  return RC_OK;
+}
+
+rc_status rc_set_quant_weights(rc_ctx *c, const rc_quant_layer *layers) {
+  g_err.clear();
+  RC_CHECK(c, RC_ERR_INVALID_ARG, "ctx is null");
+  RC_CHECK(c->esz == 2, RC_ERR_UNSUPPORTED, "8-bit weights need bf16 storage");
+  if (!layers) {
+    c->quant.clear();
+    return RC_OK;
+  }
+  for (int l = 0; l < c->L; ++l) {
+    const rc_quant_layer &q = layers[l];
+    const rc_qmat *mats[] = {&q.qkv_w, &q.fc1_w, &q.fc2_w};
+    const int rows[] = {3 * c->C, c->F, c->C}, cols[] = {c->C, c->C, c->F};
+    for (int i = 0; i < 3; ++i) {
+      RC_TRY(check_qmat(mats[i], "an 8-bit weight"));
+      RC_CHECK(mats[i]->rows == rows[i] && mats[i]->cols == cols[i] && mats[i]->block_rows == rc::kQBlock, RC_ERR_SHAPE,
+               "layer %d: an 8-bit weight is %d x %d in blocks of %d rows, not %d x %d of %d", l, mats[i]->rows, mats[i]->cols,
+               mats[i]->block_rows, rows[i], cols[i], rc::kQBlock);
+    }
+    for (const float *v : {c->layers[l].qkv_b, c->layers[l].fc1_b, c->layers[l].fc2_b, c->layers[l].sst})
+      RC_CHECK(aligned16(v), RC_ERR_ALIGN, "layer %d: 8-bit products need 16-byte aligned biases and modulation tables", l);
+  }
+  c->quant.assign(layers, layers + c->L);
+  return RC_OK;
+}
+
+rc_status rc_build_cache_quant(rc_ctx *c, const rc_cache_view *cache, int32_t step, const rc_step_io *io, void *ws,
+                               size_t ws_bytes, void *stream) {
+  g_err.clear();
+  RC_CHECK(c, RC_ERR_INVALID_ARG, "ctx is null");
+  RC_CHECK(c->esz == 2, RC_ERR_UNSUPPORTED, "the 8-bit pool needs bf16 storage");
+  RC_TRY(check_cache(c, cache, step, true));
+  RC_TRY(check_io(c, io));
+  RC_TRY(check_guided(io, cache->batch, nullptr));
+  RC_CHECK((long)cache->batch * c->N <= kMaxQRows, RC_ERR_SHAPE, "batch too large");
+  RC_CHECK(device_present(), RC_ERR_NO_DEVICE, "no HIP device");
+  return run_step<bf16>(c, cache, step, io, true, nullptr, nullptr, true, ws, ws_bytes, (hipStream_t)stream, nullptr, true);
+}
+
+rc_status rc_reuse_step_quant(rc_ctx *c, const rc_cache_view *cache, int32_t step, const rc_active_set *active,
+                              const rc_step_io *io, uint32_t flags, void *ws, size_t ws_bytes, void *stream) {
+  g_err.clear();
+  RC_CHECK(c, RC_ERR_INVALID_ARG, "ctx is null");
+  RC_CHECK(c->esz == 2, RC_ERR_UNSUPPORTED, "the 8-bit pool needs bf16 storage");
+  RC_TRY(check_cache(c, cache, step, true));
+  RC_TRY(check_io(c, io));
+  RC_TRY(check_active(c, cache, active));
+  RC_TRY(check_guided(io, cache->batch, active));
+  RC_CHECK((flags & ~(RC_FUSE_UPDATE | RC_VALIDATE)) == 0, RC_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+  RC_CHECK(flags & RC_FUSE_UPDATE, RC_ERR_UNSUPPORTED, "an 8-bit pool is updated in place (RC_FUSE_UPDATE)");
+  RC_CHECK(active->offsets_host[cache->batch] <= kMaxQRows, RC_ERR_SHAPE, "too many active tokens");
+  if (flags & RC_VALIDATE)
+    RC_CHECK(ws && aligned16(ws) && ws_bytes >= 16, RC_ERR_INVALID_ARG, "RC_VALIDATE needs the workspace");
+  RC_CHECK(device_present(), RC_ERR_NO_DEVICE, "no HIP device");
+  hipStream_t s = (hipStream_t)stream;
+  if (flags & RC_VALIDATE) RC_TRY(validate_active(c, active, (int *)ws, s));
+  return run_step<bf16>(c, cache, step, io, false, active, nullptr, true, ws, ws_bytes, s, nullptr, true);
+}
+
 rc_status rc_localize_region(rc_ctx *c, const float *maps, int32_t batch, int32_t n_delta, float threshold,
                              int32_t radius, uint8_t *mask, int32_t *idx, int32_t *offsets, int32_t *offsets_host,
                              void *stream) {
@@ -1378,6 +1588,7 @@ rc_status rc_qcache_attention(const rc_qcache *cache, const rc_active_set *rows,
   a.part = (float *)scratch;
   a.ml = (float *)((char *)scratch + qattention_part_bytes(p, R, cache->heads));
   RC_HIP(rc::launch_qattention(a, cache->batch, max_rows, p.qh, (hipStream_t)stream));
+  RC_HIP(rc::launch_qattention_combine(a, (hipStream_t)stream));
   return RC_OK;
 }
 

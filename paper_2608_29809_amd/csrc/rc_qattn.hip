@@ -620,7 +620,7 @@ QAttnPlan plan_qattention(const int *offsets, int chains, int heads, int tokens)
       qtiles += (offsets[b + 1] - offsets[b] + bq - 1) / bq;
       full += offsets[b + 1] > offsets[b];
     }
-    for (int sp = 1; sp <= std::min(n_tiles, kQMaxSplits) && (sp == 1 || rows * heads * sp <= (1L << 18)); ++sp) {
+    for (int sp = 1; sp <= std::min(n_tiles, kQMaxSplits) && (sp == 1 || rows * heads * sp <= kQMaxSplitRows); ++sp) {
       const double wgs = (double)qtiles * heads * sp, tiles = (n_tiles + sp - 1) / sp;
       double us = sp > 1 ? 4.0 + rows * heads * kHeadDim * 4.0 * (sp + 1) / 4e6 : 0.0;
       if (qh == 0)
@@ -653,10 +653,13 @@ hipError_t launch_qattention(const QAttnArgs &args, int chains, int max_rows, in
   if (qh == 0) rc_launch(qattn_few_kernel, grid, dim3(256), 0, s, a);
   else if (qh == 2) rc_launch(qattn_kernel<2>, grid, dim3(256), 0, s, a);
   else rc_launch(qattn_kernel<1>, grid, dim3(256), 0, s, a);
-  if (a.splits > 1) {
-    const long long n = (long long)a.total_rows * a.c.heads * (kHeadDim / 4);
-    rc_launch(qattn_combine_kernel, dim3((unsigned)((n + 63) / 64)), dim3(64), 0, s, a);
-  }
+  return hipGetLastError();
+}
+
+hipError_t launch_qattention_combine(const QAttnArgs &a, hipStream_t s) {
+  if (a.total_rows <= 0 || a.splits <= 1) return hipSuccess;
+  const long long n = (long long)a.total_rows * a.c.heads * (kHeadDim / 4);
+  rc_launch(qattn_combine_kernel, dim3((unsigned)((n + 63) / 64)), dim3(64), 0, s, a);
   return hipGetLastError();
 }
 

@@ -31,6 +31,27 @@ struct QuantArgs {
 };
 template <typename T> hipError_t launch_quantize(const QuantArgs &a, int block_rows, hipStream_t s);
 
+// A step's rows between two 8-bit products, one pass over each: the product of
+// the MLP's second matrix joins the residual stream and the cached hidden
+// state (y set), and the LayerNorm + modulation for the next product leaves in
+// 8 bits (q set).
+struct NormQuantArgs {
+  float *X;                 // [rows][C]
+  int rows, C;
+  const float *y;           // [rows][C] or null; X += (gate + gate2) (y + bias)
+  const float *bias, *gate, *gate2;
+  const int *packed;        // packed (chain << 16) | token per row
+  bf16 *hslot;              // H of chain 0's slot
+  long long chain_stride;   // elements
+  const float *sst, *t0;    // shift and scale: rows shift_row and shift_row + 1 of sst + t0
+  int shift_row;
+  float eps;
+  uint8_t *q;               // [rows][C] or null
+  uint8_t *scales;          // [C / 128][scale_ld]
+  int scale_ld;
+};
+hipError_t launch_norm_quantize(const NormQuantArgs &a, hipStream_t s);
+
 struct QGemmArgs {
   const uint8_t *a, *w;     // [M][K], [N][K]
   const uint8_t *as, *ws;   // scales: [K blocks][as_ld], [K blocks][ws_ld]
@@ -65,7 +86,7 @@ __device__ __forceinline__ int2 chain_rows(const ChainRows &a, int b) {
 struct QStoreArgs {
   QCacheArgs c;
   ChainRows rows;
-  const int *idx;
+  const int *idx;           // or null: every token of every chain
   const void *k, *v;        // [rows][heads * 72]
   long long ld;             // elements
 };
@@ -87,9 +108,11 @@ struct QAttnArgs {
   int total_rows;
 };
 constexpr int kQMaxSplits = 16;
+constexpr long kQMaxSplitRows = 1L << 18;  // rows x heads x splits of a split plan
 struct QAttnPlan { int qh, splits; };  // qh: 32-query halves per wave, or 0: 16 queries per workgroup
 QAttnPlan plan_qattention(const int *offsets, int chains, int heads, int tokens);
 hipError_t launch_qattention(const QAttnArgs &a, int chains, int max_rows, int qh, hipStream_t s);
+hipError_t launch_qattention_combine(const QAttnArgs &a, hipStream_t s);  // (splits > 1)
 
 // ------------------------------------------------------------------ device side
 

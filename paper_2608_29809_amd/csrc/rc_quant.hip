@@ -92,6 +92,72 @@ template <typename T> hipError_t launch_quantize(const QuantArgs &a, int block_r
 template hipError_t launch_quantize<bf16>(const QuantArgs &, int, hipStream_t);
 template hipError_t launch_quantize<float>(const QuantArgs &, int, hipStream_t);
 
+// One workgroup per row; a block of 128 columns is 32 lanes of four.
+__global__ __launch_bounds__(256) void norm_quantize_kernel(NormQuantArgs a) {
+  __shared__ float red[4];
+  const int r = blockIdx.x, t = threadIdx.x, C4 = a.C >> 2;
+  constexpr int MAXV = 2;  // C <= 4 * 256 * MAXV
+  float *X = a.X + (size_t)r * a.C;
+  const f32x4 zero4 = {0.0f, 0.0f, 0.0f, 0.0f};
+  f32x4 x[MAXV], shift[MAXV], scale[MAXV];
+  const float *sh = a.sst + (size_t)a.shift_row * a.C, *tsh = a.t0 + (size_t)a.shift_row * a.C;
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < MAXV; ++i) {
+    const int n = (t + 256 * i) * 4;
+    x[i] = shift[i] = scale[i] = zero4;
+    if (n >= a.C) continue;
+    x[i] = *(const f32x4 *)(X + n);
+    if (a.q) {
+      shift[i] = *(const f32x4 *)(sh + n) + *(const f32x4 *)(tsh + n);
+      scale[i] = *(const f32x4 *)(sh + a.C + n) + *(const f32x4 *)(tsh + a.C + n);
+    }
+    if (a.y) {
+      const f32x4 y = *(const f32x4 *)(a.y + (size_t)r * a.C + n) + *(const f32x4 *)(a.bias + n);
+      const f32x4 g = *(const f32x4 *)(a.gate + n) + *(const f32x4 *)(a.gate2 + n);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i][e] += g[e] * y[e];
+      *(f32x4 *)(X + n) = x[i];
+      const int pk = a.packed[r];
+      *(bf16x4 *)(a.hslot + row_chain(pk) * a.chain_stride + (size_t)row_token(pk) * a.C + n) =
+          bf16x4{(bf16)x[i][0], (bf16)x[i][1], (bf16)x[i][2], (bf16)x[i][3]};
+    }
+    s += (x[i][0] + x[i][1]) + (x[i][2] + x[i][3]);
+  }
+  if (!a.q) return;
+  const float mean = block4_sum(s, red) / a.C;
+  float d2 = 0.0f;
+#pragma unroll
+  for (int i = 0; i < MAXV; ++i)
+    if (t + 256 * i < C4)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) d2 += (x[i][e] - mean) * (x[i][e] - mean);
+  const float rstd = rsqrtf(block4_sum(d2, red) / a.C + a.eps);
+#pragma unroll
+  for (int i = 0; i < MAXV; ++i) {
+    const int n = (t + 256 * i) * 4;
+    float v[4], m = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = (x[i][e] - mean) * rstd * (1.0f + scale[i][e]) + shift[i][e];
+      m = fmaxf(m, q_magnitude(v[e]));
+    }
+    m = row16_max(m);
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    const int e8 = q_exponent(m);
+    if (n >= a.C) continue;
+    *(uint32_t *)(a.q + (size_t)r * a.C + n) = q_pack4(v, q_inverse(e8));
+    if ((t & 31) == 0) a.scales[(size_t)(n / kQBlock) * a.scale_ld + r] = (uint8_t)e8;
+  }
+}
+
+hipError_t launch_norm_quantize(const NormQuantArgs &a, hipStream_t s) {
+  if (a.rows <= 0) return hipSuccess;
+  if (a.C % kQBlock || a.C > 2048) return hipErrorInvalidValue;
+  rc_launch(norm_quantize_kernel, dim3(a.rows), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
 // ------------------------------------------------------------------ cache store
 
 // First position in [lo, hi) of an ascending list whose entry is >= key: the
@@ -120,12 +186,16 @@ template <typename T> __global__ __launch_bounds__(192) void qcache_store_kernel
   __shared__ float red[3];
   const int tid = threadIdx.x, blk = blockIdx.x, head = blockIdx.y >> 1, which = blockIdx.y & 1, b = blockIdx.z;
   const int2 rr = chain_rows(a.rows, b);
-  const int lo = wave_lower_bound(a.idx, rr.x, rr.y, blk * kQTokens);
-  const int hi = wave_lower_bound(a.idx, lo, min(rr.y, lo + kQTokens), (blk + 1) * kQTokens);
-  if (lo >= hi) return;
-  if (tid < kQTokens) row_of[tid] = -1;
-  __syncthreads();
-  if (tid < hi - lo) row_of[a.idx[lo + tid] & (kQTokens - 1)] = lo + tid;
+  if (a.idx) {
+    const int lo = wave_lower_bound(a.idx, rr.x, rr.y, blk * kQTokens);
+    const int hi = wave_lower_bound(a.idx, lo, min(rr.y, lo + kQTokens), (blk + 1) * kQTokens);
+    if (lo >= hi) return;
+    if (tid < kQTokens) row_of[tid] = -1;
+    __syncthreads();
+    if (tid < hi - lo) row_of[a.idx[lo + tid] & (kQTokens - 1)] = lo + tid;
+  } else if (tid < kQTokens) {
+    row_of[tid] = rr.x + blk * kQTokens + tid;
+  }
   __syncthreads();
   const size_t tile = ((size_t)head * (a.c.tokens / kQTokens) + blk) * 2 + which;
   uint8_t *data = a.c.data + b * a.c.chain_stride + tile * kQTileBytes;

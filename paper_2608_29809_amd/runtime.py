@@ -19,6 +19,7 @@ import torch
 from . import abi
 
 GLOBAL_MATS = ("pe_w", "temb_w1", "temb_w2", "tblock_w", "cap_w1", "cap_w2", "fin_w")
+QUANT_MATS = ("qkv_w", "fc1_w", "fc2_w")
 LAYER_MATS = ("qkv_w", "proj_w", "xq_w", "xkv_w", "xproj_w", "fc1_w", "fc2_w")
 
 
@@ -58,14 +59,22 @@ class ActiveSet:
 class CacheBuffer:
     """The cache pool: device memory, or with host=True pinned host memory
     (the host-resident pool of the pipelined step; accessors then return
-    host tensors)."""
+    host tensors), or with bits=8 device memory with keys and values in 8 bits
+    (`quant` gives a slot's; it starts as zeros)."""
 
-    def __init__(self, model: "RegionCacheModel", batch: int, steps: int, host: bool = False):
-        nbytes = abi.rc_cache_bytes(model.ctx, batch, steps)
+    def __init__(self, model: "RegionCacheModel", batch: int, steps: int, host: bool = False, bits: int = 16):
+        if bits not in (8, 16):
+            raise ValueError(f"bits {bits} is not 8 or 16")
+        if bits == 8 and (host or model.dtype != torch.bfloat16):
+            raise ValueError("an 8-bit pool is in device memory, of a bf16 model")
+        nbytes = (abi.rc_quant_cache_bytes if bits == 8 else abi.rc_cache_bytes)(model.ctx, batch, steps)
         self.model = model
         self.host = host
+        self.bits = bits
         if host:
             self.buf = torch.empty(nbytes, dtype=torch.uint8, pin_memory=True)
+        elif bits == 8:
+            self.buf = torch.zeros(nbytes, dtype=torch.uint8, device=model.device)
         else:
             self.buf = torch.empty(nbytes, dtype=torch.uint8, device=model.device)
         self.view = abi.rc_cache_view(self.buf.data_ptr(), nbytes, batch, steps)
@@ -76,17 +85,35 @@ class CacheBuffer:
         return self.buf[off:off + n * esz].view(dtype)
 
     def offsets(self, b, t, l):
+        """Byte offsets of a slot's keys, values and hidden state (bits=8: keys and values, scales, hidden state)."""
         k, v, h = C.c_size_t(), C.c_size_t(), C.c_size_t()
-        abi.rc_cache_offsets(self.model.ctx, C.byref(self.view), b, t, l, C.byref(k), C.byref(v), C.byref(h))
+        f = abi.rc_quant_cache_offsets if self.bits == 8 else abi.rc_cache_offsets
+        f(self.model.ctx, C.byref(self.view), b, t, l, C.byref(k), C.byref(v), C.byref(h))
         return k.value, v.value, h.value
+
+    def quant(self, t, l):
+        """Keys and values of every chain's slot (t, l) as a QuantCache (bits=8)."""
+        from .quant import QuantCache
+        if self.bits != 8:
+            raise ValueError("the pool is not in 8 bits")
+        m = self.model
+        data, scales, _ = self.offsets(0, t, l)
+        apart = self.offsets(1, t, l)[0] - data if self.batch > 1 else 0
+        shape, tile = (self.batch, m.H, m.N // 64, 2, 64, 72), 64 * 72
+        return QuantCache(self.buf.as_strided(shape, (apart, m.N * 144, 2 * tile, tile, 72, 1), data).view(torch.float8_e4m3fn),
+                          self.buf.as_strided(shape[:4], (apart, m.N // 32, 2, 1), scales))
 
     def K(self, b, t, l):
         """Keys of slot (b, t, l) as [heads, N, 72]."""
+        if self.bits == 8:
+            raise ValueError("keys in 8 bits: use quant(t, l)")
         m = self.model
         return self._typed(self.offsets(b, t, l)[0], m.H * m.N * 72, m.dtype).view(m.H, m.N, 72)
 
     def V(self, b, t, l):
         """Values of slot (b, t, l) as [heads, N, 72] (token-major, like the keys)."""
+        if self.bits == 8:
+            raise ValueError("values in 8 bits: use quant(t, l)")
         m = self.model
         return self._typed(self.offsets(b, t, l)[1], m.H * m.N * 72, m.dtype).view(m.H, m.N, 72)
 
@@ -98,7 +125,7 @@ class CacheBuffer:
     def latent(self, b, t):
         m = self.model
         off = C.c_size_t()
-        abi.rc_cache_latent_offset(m.ctx, C.byref(self.view), b, t, C.byref(off))
+        (abi.rc_quant_cache_latent_offset if self.bits == 8 else abi.rc_cache_latent_offset)(m.ctx, C.byref(self.view), b, t, C.byref(off))
         Hl, Wl = m.shape.grid_h * 2, m.shape.grid_w * 2
         return self._typed(off.value, 4 * Hl * Wl, torch.float32).view(4, Hl, Wl)
 
@@ -126,9 +153,14 @@ class RegionCacheModel:
             return t.data_ptr()
 
         layers = (abi.rc_layer_weights * shape.layers)()
+        self._quantizable = []  # the matrices that quantize_weights takes, per block
         for i, lw in enumerate(weights["layers"]):
+            kept = {}
             for f in abi.LAYER_FIELDS:
                 setattr(layers[i], f, mat(lw[f]) if f in LAYER_MATS else vec(lw[f]))
+                if f in QUANT_MATS:
+                    kept[f] = self._keep[-1]
+            self._quantizable.append(kept)
         self._layers = layers
         w = abi.rc_weights()
         w.layers = C.cast(layers, C.POINTER(abi.rc_layer_weights))
@@ -157,8 +189,24 @@ class RegionCacheModel:
             pass
 
     # ------------------------------------------------------------ buffers
-    def alloc_cache(self, batch: int, steps: int, host: bool = False) -> CacheBuffer:
-        return CacheBuffer(self, batch, steps, host)
+    def alloc_cache(self, batch: int, steps: int, host: bool = False, bits: int = 16) -> CacheBuffer:
+        return CacheBuffer(self, batch, steps, host, bits)
+
+    def quantize_weights(self, enable: bool = True):
+        """Steps on an 8-bit pool take the QKV and MLP products from 8-bit
+        weights (made here, once), or with enable=False from the bf16 ones again."""
+        from .quant import quantize
+        if not enable:
+            abi.rc_set_quant_weights(self.ctx, None)
+            self._quant = None
+            return
+        keep, layers = [], (abi.rc_quant_layer * self.L)()
+        for i, mats in enumerate(self._quantizable):
+            for f, t in mats.items():
+                keep.append(quantize(t, 128))
+                setattr(layers[i], f, keep[-1].struct())
+        abi.rc_set_quant_weights(self.ctx, layers)
+        self._quant = keep
 
     def staging(self, batch: int) -> torch.Tensor:
         """Device staging ring of the host-resident pool."""
@@ -167,8 +215,8 @@ class RegionCacheModel:
             self._stage = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         return self._stage
 
-    def workspace(self, max_rows: int, batch: int) -> torch.Tensor:
-        nbytes = abi.rc_workspace_bytes(self.ctx, max_rows, batch)
+    def workspace(self, max_rows: int, batch: int, bits: int = 16) -> torch.Tensor:
+        nbytes = (abi.rc_quant_workspace_bytes if bits == 8 else abi.rc_workspace_bytes)(self.ctx, max_rows, batch)
         if self._ws is None or self._ws.numel() < nbytes:
             self._ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         return self._ws
@@ -208,11 +256,13 @@ class RegionCacheModel:
         the conditional and unconditional branch of one image."""
         io, keep = self._io(inp, timestep, timestep_next, tkv, delta, maps, latent_out, t_vec, text_valid,
                             guidance)
-        ws = self.workspace(cache.batch * self.N, cache.batch)
+        ws = self.workspace(cache.batch * self.N, cache.batch, cache.bits)
         if cache.host:
             st = self.staging(cache.batch)
             abi.rc_build_cache_hosted(self.ctx, C.byref(cache.view), step, C.byref(io), _ptr(st), st.numel(),
                                       _ptr(ws), ws.numel(), _stream())
+        elif cache.bits == 8:
+            abi.rc_build_cache_quant(self.ctx, C.byref(cache.view), step, C.byref(io), _ptr(ws), ws.numel(), _stream())
         else:
             abi.rc_build_cache(self.ctx, C.byref(cache.view), step, C.byref(io), _ptr(ws), ws.numel(), _stream())
 
@@ -224,7 +274,7 @@ class RegionCacheModel:
         an invalid set raises RcError (RC_ERR_INDEX) before any launch."""
         io, keep = self._io(inp, timestep, timestep_next, tkv, delta, maps, latent_out, t_vec, text_valid,
                             guidance)
-        ws = self.workspace(max(act.total, 1), cache.batch)
+        ws = self.workspace(max(act.total, 1), cache.batch, cache.bits)
         s = act.struct()
         if cache.host:
             if not fuse or active_hidden is not None:
@@ -232,6 +282,12 @@ class RegionCacheModel:
             st = self.staging(cache.batch)
             abi.rc_reuse_step_hosted(self.ctx, C.byref(cache.view), step, C.byref(s), C.byref(io), _ptr(st),
                                      st.numel(), _ptr(ws), ws.numel(), _stream())
+        elif cache.bits == 8:
+            if not fuse or active_hidden is not None:
+                raise ValueError("an 8-bit pool is updated in place (fuse=True, no active_hidden)")
+            flags = abi.RC_FUSE_UPDATE | (abi.RC_VALIDATE if validate else 0)
+            abi.rc_reuse_step_quant(self.ctx, C.byref(cache.view), step, C.byref(s), C.byref(io), flags, _ptr(ws),
+                                    ws.numel(), _stream())
         else:
             flags = (abi.RC_FUSE_UPDATE if fuse else 0) | (abi.RC_VALIDATE if validate else 0)
             abi.rc_reuse_step(self.ctx, C.byref(cache.view), step, C.byref(s), C.byref(io), _ptr(active_hidden),
@@ -246,6 +302,8 @@ class RegionCacheModel:
         abi.rc_validate_active(self.ctx, C.byref(s), act.batch, _ptr(scratch), scratch.numel(), _stream())
 
     def update_cache(self, cache: CacheBuffer, step: int, act: ActiveSet, active_hidden: torch.Tensor):
+        if cache.bits == 8:
+            raise ValueError("an 8-bit pool is updated in place by its steps")
         s = act.struct()
         abi.rc_update_cache(self.ctx, C.byref(cache.view), step, C.byref(s), _ptr(active_hidden), _stream())
 

@@ -86,8 +86,9 @@ class EditSession:
 
     def __init__(self, model: RegionCacheModel, batch: int, T: int = 20, rho: float = 0.2, tau_s: float = 0.8,
                  reading: str = "dense_then_reuse", threshold: float = 0.3, radius: int = 1,
-                 guidance: Optional[float] = None):
-        """guidance: classifier-free guidance scale; the batch then holds
+                 guidance: Optional[float] = None, cache_bits: int = 16):
+        """cache_bits: 8 keeps the pool's keys and values in 8 bits.
+        guidance: classifier-free guidance scale; the batch then holds
         (conditional, unconditional) chain pairs and the localised region of
         each conditional chain is used for its pair."""
         if reading not in ("dense_then_reuse", "paper"):
@@ -98,7 +99,7 @@ class EditSession:
         self.model, self.batch, self.T = model, batch, T
         self.rho, self.tau_s, self.reading = rho, tau_s, reading
         self.threshold, self.radius = threshold, radius
-        self.cache: CacheBuffer = model.alloc_cache(batch, T)
+        self.cache: CacheBuffer = model.alloc_cache(batch, T, bits=cache_bits)
         self.tgrid = timestep_grid(T)
         self.turns = 0
         self.prev_txt: Optional[torch.Tensor] = None

@@ -38,13 +38,11 @@ def amax_finite(x, axis):
 def quantize(x, tile):
     """Values (e4m3 numbers) and scale bytes [column blocks][row blocks]."""
     x = np.asarray(x, np.float64)
-    q, e = np.empty_like(x), np.empty((-(-x.shape[1] // 128), -(-x.shape[0] // tile)), np.int64)
-    for j in range(e.shape[0]):
-        for i in range(e.shape[1]):
-            s = np.s_[i * tile:(i + 1) * tile, j * 128:(j + 1) * 128]
-            e[j, i] = scale_byte(amax_finite(x[s], None))
-            q[s] = round_e4m3(x[s] * 2.0 ** (127.0 - e[j, i]))
-    return q, e
+    rows, cols = x.shape
+    padded = np.pad(x, ((0, -rows % tile), (0, -cols % 128)))
+    e = scale_byte(amax_finite(padded.reshape(-1, tile, padded.shape[1] // 128, 128), (1, 3)).T)
+    f = np.repeat(np.repeat(2.0 ** (127.0 - e).T, tile, 0)[:rows], 128, 1)[:, :cols]
+    return round_e4m3(x * f), e
 
 
 def dequantize(q, e, tile):

@@ -151,6 +151,103 @@ def test_attention_refusals():
         assert call(good) == -6
 
 
+# ------------------------------------------------------------------ steps on an 8-bit pool
+
+def make_ctx(dtype=abi.RC_BF16, layers=2):
+    L = (abi.rc_layer_weights * layers)()
+    for i in range(layers):
+        for f in abi.LAYER_FIELDS:
+            setattr(L[i], f, FAKE)
+    w = abi.rc_weights()
+    w.layers = C.cast(L, C.POINTER(abi.rc_layer_weights))
+    for f in abi.GLOBAL_FIELDS:
+        setattr(w, f, FAKE)
+    cfg = abi.rc_model_config(1152, 16, 72, 4608, layers, 120, 4096, 32, 32, 4, 2, 8, dtype, 0, 1e-6)
+    ctx = C.c_void_p()
+    assert abi.LIB.rc_create(C.byref(cfg), C.byref(w), C.byref(ctx)) == 0
+    return ctx, L
+
+
+def step_io(**over):
+    d = dict(input=FAKE, t_vec=None, timestep=500, timestep_next=450, text_kv=FAKE, delta_cols_host=None,
+             n_delta=0, maps=None, latent_out=FAKE, text_valid=None, guided=0, guidance_scale=0.0)
+    d.update(over)
+    return abi.rc_step_io(*[d[f] for f, _ in abi.rc_step_io._fields_])
+
+
+def test_pool_sizes_and_offsets():
+    ctx, keep = make_ctx()
+    N, C_, L = 1024, 1152, 2
+    scales = 16 * (N // 64) * 2
+    slot = 2 * N * C_ + scales + 2 * N * C_
+    assert scales % 256 == 0 and abi.rc_quant_cache_bytes(ctx, 3, 5) == 3 * 5 * L * slot + 3 * 6 * 4 * 64 * 64 * 4
+    view = abi.rc_cache_view(FAKE, abi.rc_quant_cache_bytes(ctx, 3, 5), 3, 5)
+    d, sc, h = C.c_size_t(), C.c_size_t(), C.c_size_t()
+    abi.rc_quant_cache_offsets(ctx, C.byref(view), 2, 4, 1, C.byref(d), C.byref(sc), C.byref(h))
+    base = ((2 * 5 + 4) * L + 1) * slot
+    assert (d.value, sc.value, h.value) == (base, base + 2 * N * C_, base + 2 * N * C_ + scales)
+    abi.rc_quant_cache_latent_offset(ctx, C.byref(view), 1, 5, C.byref(d))
+    assert d.value == 3 * 5 * L * slot + (6 + 5) * 4 * 64 * 64 * 4
+    with pytest.raises(abi.RcError):
+        abi.rc_quant_cache_offsets(ctx, C.byref(view), 3, 0, 0, C.byref(d), None, None)
+    assert abi.rc_quant_workspace_bytes(ctx, 500, 1) > abi.rc_workspace_bytes(ctx, 500, 1)
+    assert abi.rc_quant_cache_bytes(ctx, 0, 5) == 0 and abi.rc_quant_workspace_bytes(ctx, 5, 0) == 0
+    f32, keep2 = make_ctx(abi.RC_F32)
+    assert abi.rc_quant_cache_bytes(f32, 1, 1) == 0 and abi.rc_quant_workspace_bytes(f32, 1, 1) == 0
+    abi.rc_destroy(ctx)
+    abi.rc_destroy(f32)
+
+
+def test_quant_step_refusals():
+    ctx, keep = make_ctx()
+    nb, ws = abi.rc_quant_cache_bytes(ctx, 2, 4), abi.rc_quant_workspace_bytes(ctx, 2048, 2)
+    view, a, io = abi.rc_cache_view(FAKE, nb, 2, 4), aset([0, 10, 20]), step_io()
+    build, step = abi.LIB.rc_build_cache_quant, abi.LIB.rc_reuse_step_quant
+    fuse = abi.RC_FUSE_UPDATE
+    assert build(None, C.byref(view), 0, C.byref(io), FAKE, ws, None) == -1
+    assert build(ctx, C.byref(view), 4, C.byref(io), FAKE, ws, None) == -2
+    assert build(ctx, C.byref(abi.rc_cache_view(FAKE, nb - 1, 2, 4)), 0, C.byref(io), FAKE, ws, None) == -5
+    assert build(ctx, C.byref(view), 0, C.byref(step_io(timestep=1000)), FAKE, ws, None) == -1
+    assert step(ctx, C.byref(view), 1, C.byref(a), C.byref(io), 0, FAKE, ws, None) == -8       # not in place
+    assert step(ctx, C.byref(view), 1, C.byref(a), C.byref(io), fuse | 4, FAKE, ws, None) == -1
+    assert step(ctx, C.byref(view), 1, C.byref(aset([0, 10, 5])), C.byref(io), fuse, FAKE, ws, None) == -4
+    assert step(ctx, C.byref(view), 1, C.byref(aset([0, 2000, 2001])), C.byref(io), fuse, FAKE, ws, None) == -4
+    assert step(ctx, C.byref(view), 1, C.byref(a), C.byref(io), fuse | abi.RC_VALIDATE, FAKE, 8, None) == -1
+    f32, keep2 = make_ctx(abi.RC_F32)
+    assert build(f32, C.byref(view), 0, C.byref(io), FAKE, ws, None) == -8
+    assert step(f32, C.byref(view), 1, C.byref(a), C.byref(io), fuse, FAKE, ws, None) == -8
+    if NO_GPU:
+        assert build(ctx, C.byref(view), 0, C.byref(io), FAKE, ws, None) == -6
+        assert step(ctx, C.byref(view), 1, C.byref(a), C.byref(io), fuse, FAKE, ws, None) == -6
+    abi.rc_destroy(ctx)
+    abi.rc_destroy(f32)
+
+
+def test_quant_weight_refusals():
+    ctx, keep = make_ctx()
+
+    def layers(**over):
+        q = (abi.rc_quant_layer * 2)()
+        for i in range(2):
+            q[i].qkv_w = qmat(rows=3456, cols=1152, ld=1152, scale_ld=32, block_rows=128)
+            q[i].fc1_w = qmat(rows=4608, cols=1152, ld=1152, scale_ld=48, block_rows=128)
+            q[i].fc2_w = qmat(rows=1152, cols=4608, ld=4608, scale_ld=16, block_rows=128)
+        for k, v in over.items():
+            setattr(q[1], k, v)
+        return q
+
+    put = abi.LIB.rc_set_quant_weights
+    assert put(ctx, layers()) == 0 and put(ctx, None) == 0
+    assert put(None, layers()) == -1
+    assert put(ctx, layers(fc1_w=qmat(rows=4608, cols=1152, ld=1152, scale_ld=4608))) == -2             # a scale per row
+    assert put(ctx, layers(fc2_w=qmat(rows=4608, cols=1152, ld=1152, scale_ld=48, block_rows=128))) == -2
+    assert put(ctx, layers(qkv_w=qmat(rows=3456, cols=1152, ld=1152, scale_ld=32, block_rows=128, data=None))) == -1
+    f32, keep2 = make_ctx(abi.RC_F32)
+    assert put(f32, layers()) == -8
+    abi.rc_destroy(ctx)
+    abi.rc_destroy(f32)
+
+
 def test_python_refusals():
     f8 = torch.float8_e4m3fn
     with pytest.raises(ValueError, match="GPU"):

@@ -179,7 +179,7 @@ size_t quant_cache_bytes(const rc_ctx *c, int B, int T) {
 
 // What a step on an 8-bit pool needs behind the workspace of an ordinary one.
 struct QuantWs {
-  size_t qkv, a, as, g, gs, y, part, total;
+  size_t qkv, a, as, g, gs, part, total;
   int scale_ld;
 };
 QuantWs quant_ws(const rc_ctx *c, int max_rows) {
@@ -193,7 +193,6 @@ QuantWs quant_ws(const rc_ctx *c, int max_rows) {
   w.as = take((size_t)(c->C / rc::kQBlock) * w.scale_ld);
   w.g = take(R * c->F);
   w.gs = take((size_t)(c->F / rc::kQBlock) * w.scale_ld);
-  w.y = take(R * c->C * sizeof(float));
   const size_t split = std::min(R * c->H * rc::kQMaxSplits, (size_t)rc::kQMaxSplitRows);
   w.part = take(split * (rc::kHeadDim + 2) * sizeof(float) + 256);
   w.total = o;
@@ -551,20 +550,18 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
   // 8-bit pool: the layer's products and attention
   char *qws = wsb + wl.total;
   uint8_t *qa = (uint8_t *)(qws + qw.a), *qas = (uint8_t *)(qws + qw.as);
-  auto norm_quant = [&](int cls, int l, int shift_row, const rc::NormQuantArgs &with) -> rc_status {
-    rc::NormQuantArgs a = with;
-    a.X = X; a.rows = R; a.C = C; a.eps = c->cfg.ln_eps; a.t0 = t0; a.shift_row = shift_row;
-    a.sst = c->layers[std::min(l, L - 1)].sst;
-    if (l < L) { a.q = qa; a.scales = qas; a.scale_ld = qw.scale_ld; }
-    return timed(c, cls, s, [&] { return rc::launch_norm_quantize(a, s); });
+  auto norm_quant = [&](int l, int shift_row) -> rc_status {
+    rc::NormQuantArgs a{};
+    a.X = X; a.rows = R; a.C = C; a.eps = c->cfg.ln_eps; a.sst = c->layers[l].sst; a.t0 = t0; a.shift_row = shift_row;
+    a.q = qa; a.scales = qas; a.scale_ld = qw.scale_ld;
+    return timed(c, RC_KC_NORM, s, [&] { return rc::launch_norm_quantize(a, s); });
   };
-  auto qgemm = [&](int cls, const uint8_t *a, const uint8_t *as, const rc_qmat &w, const float *bias, bool gelu, bool f32,
-                   void *out) -> rc_status {
-    rc::QGemmArgs g{};
+  auto qgemm = [&](int cls, rc::QGemmArgs g, const uint8_t *a, const uint8_t *as, const rc_qmat &w, const float *bias,
+                   rc::QGemmEpi epi) -> rc_status {
     g.a = a; g.as = as; g.lda = w.cols; g.as_ld = qw.scale_ld;
     g.w = (const uint8_t *)w.data; g.ws = w.scales; g.ldw = w.ld; g.ws_ld = w.scale_ld;
-    g.M = R; g.N = w.rows; g.K = w.cols; g.bias = bias; g.out = out; g.ldo = w.rows;
-    return timed(c, cls, s, [&] { return rc::launch_qgemm(g, rc::plan_qgemm(g.M, g.N, g.K), gelu, f32, s); });
+    g.M = R; g.N = w.rows; g.K = w.cols; g.bias = bias; g.ldo = w.rows;
+    return timed(c, cls, s, [&] { return rc::launch_qgemm(g, rc::plan_qgemm(g.M, g.N, g.K, epi), epi, false, s); });
   };
   rc::ChainRows q_rows{};
   rc::QAttnPlan q_plan{1, 1};
@@ -622,14 +619,16 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
     }
 
     if (!a1_ready) {
-      if (q_mm) RC_TRY(norm_quant(RC_KC_NORM, l, 0, rc::NormQuantArgs{}));
+      if (q_mm) RC_TRY(norm_quant(l, 0));
       else RC_TRY(timed(c, RC_KC_NORM, s, [&] { return rc::launch_ln_mod<T>(X, R, C, lw.sst, t0, 0, c->cfg.ln_eps, A1, s); }));
     }
     a1_ready = false;
     if (quant) {  // QKV rows, keys and values merged into the 8-bit slot, attention over the whole slot
       bf16 *qkv = (bf16 *)(qws + qw.qkv);  // [R][3C]
       if (q_mm) {
-        RC_TRY(qgemm(RC_KC_GEMM_QKV, qa, qas, c->quant[l].qkv_w, lw.qkv_b, false, false, qkv));
+        rc::QGemmArgs g{};
+        g.out = qkv;
+        RC_TRY(qgemm(RC_KC_GEMM_QKV, g, qa, qas, c->quant[l].qkv_w, lw.qkv_b, rc::QG_STORE));
       } else {
         rc::GemmArgs g{};
         g.A = A1; g.W = lw.qkv_w; g.bias = lw.qkv_b; g.M = R; g.N = 3 * C; g.K = C; g.lda = C; g.out = qkv; g.ldo = 3 * C;
@@ -642,7 +641,7 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
       qc.heads = H; qc.tokens = N;
       rc::QStoreArgs sa{};
       sa.c = qc; sa.rows = q_rows; sa.idx = dense ? nullptr : act->idx; sa.k = qkv + C; sa.v = qkv + 2 * C; sa.ld = 3 * C;
-      RC_TRY(timed(c, RC_KC_MISC, s, [&] { return rc::launch_qcache_store<bf16>(sa, B, s); }));
+      RC_TRY(timed(c, RC_KC_MISC, s, [&] { return rc::launch_qcache_store<bf16>(sa, B, max_rb, s); }));
       rc::QAttnArgs a{};
       a.c = qc; a.rows = q_rows; a.q = qkv; a.ldq = 3 * C; a.scale_log2 = scale_log2; a.out = (bf16 *)O; a.ldo = C;
       a.splits = q_plan.splits; a.total_rows = R;
@@ -731,20 +730,15 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
       else { g.warm = lw.fc2_w; g.warm_lines = fc2_lines; }
       RC_TRY(gemm<T>(c, RC_KC_GEMM_XPROJ, g, rc::EPI_RESID, gpart, gpf, s));
     }
-    if (q_mm) {  // MLP from 8-bit weights; merge into the cached hidden state and the next block's LayerNorm in one pass
+    if (q_mm) {  // MLP from 8-bit weights, its inner activations in 8 bits; merge into the cached hidden state
       uint8_t *qg = (uint8_t *)(qws + qw.g), *qgs = (uint8_t *)(qws + qw.gs);
-      float *y = (float *)(qws + qw.y);
-      RC_TRY(norm_quant(RC_KC_NORM, l, 3, rc::NormQuantArgs{}));
-      RC_TRY(qgemm(RC_KC_GEMM_FC1, qa, qas, c->quant[l].fc1_w, lw.fc1_b, true, false, G));
-      rc::QuantArgs ga{};
-      ga.x = G; ga.ldx = F; ga.rows = R; ga.cols = F; ga.q = qg; ga.ldq = F; ga.scales = qgs; ga.scale_ld = qw.scale_ld;
-      RC_TRY(timed(c, RC_KC_MISC, s, [&] { return rc::launch_quantize<bf16>(ga, 1, s); }));
-      RC_TRY(qgemm(RC_KC_GEMM_FC2, qg, qgs, c->quant[l].fc2_w, nullptr, false, true, y));
-      rc::NormQuantArgs na{};
-      na.y = y; na.bias = lw.fc2_b; na.gate = lw.sst + 5 * C; na.gate2 = t0 + 5 * C; na.packed = rows;
-      na.hslot = (bf16 *)Hs; na.chain_stride = slot_chain_stride;
-      RC_TRY(norm_quant(RC_KC_SPLIT_FINISH, l + 1, 0, na));
-      a1_ready = true;
+      RC_TRY(norm_quant(l, 3));
+      rc::QGemmArgs up{}, down{};
+      up.out = qg; up.out_scales = qgs; up.out_scale_ld = qw.scale_ld;
+      RC_TRY(qgemm(RC_KC_GEMM_FC1, up, qa, qas, c->quant[l].fc1_w, lw.fc1_b, rc::QG_GELU8));
+      down.X = X; down.gate = lw.sst + 5 * C; down.gate2 = t0 + 5 * C; down.packed = rows;
+      down.hslot = (bf16 *)Hs; down.chain_stride = slot_chain_stride;
+      RC_TRY(qgemm(RC_KC_GEMM_FC2, down, qg, qgs, c->quant[l].fc2_w, lw.fc2_b, rc::QG_RESID));
       continue;
     }
     if (!fold_nt)
@@ -1376,8 +1370,7 @@ rc_status rc_set_quant_weights(rc_ctx *c, const rc_quant_layer *layers) {
                "layer %d: an 8-bit weight is %d x %d in blocks of %d rows, not %d x %d of %d", l, mats[i]->rows, mats[i]->cols,
                mats[i]->block_rows, rows[i], cols[i], rc::kQBlock);
     }
-    for (const float *v : {c->layers[l].qkv_b, c->layers[l].fc1_b, c->layers[l].fc2_b, c->layers[l].sst})
-      RC_CHECK(aligned16(v), RC_ERR_ALIGN, "layer %d: 8-bit products need 16-byte aligned biases and modulation tables", l);
+    RC_CHECK(aligned16(c->layers[l].sst), RC_ERR_ALIGN, "layer %d: 8-bit products need a 16-byte aligned modulation table", l);
   }
   c->quant.assign(layers, layers + c->L);
   return RC_OK;
@@ -1528,7 +1521,8 @@ rc_status rc_qgemm(const rc_qmat *a, const rc_qmat *w, const float *bias, int32_
   g.a = (const uint8_t *)a->data; g.as = a->scales; g.lda = a->ld; g.as_ld = a->scale_ld;
   g.w = (const uint8_t *)w->data; g.ws = w->scales; g.ldw = w->ld; g.ws_ld = w->scale_ld;
   g.M = a->rows; g.N = w->rows; g.K = a->cols; g.bias = bias; g.out = out; g.ldo = ldo;
-  RC_HIP(rc::launch_qgemm(g, rc::plan_qgemm(g.M, g.N, g.K), gelu != 0, out_dtype == RC_F32, (hipStream_t)stream));
+  const rc::QGemmEpi epi = gelu ? rc::QG_GELU : rc::QG_STORE;
+  RC_HIP(rc::launch_qgemm(g, rc::plan_qgemm(g.M, g.N, g.K, epi), epi, out_dtype == RC_F32, (hipStream_t)stream));
   return RC_OK;
 }
 
@@ -1547,8 +1541,12 @@ rc_status rc_qcache_store(const rc_qcache *cache, const rc_active_set *active, c
   RC_CHECK(device_present(), RC_ERR_NO_DEVICE, "no HIP device");
   rc::QStoreArgs a{};
   a.c = qcache_args(cache); a.rows = chain_rows_args(active); a.idx = active->idx; a.k = k; a.v = v; a.ld = ld;
-  RC_HIP(dtype == RC_F32 ? rc::launch_qcache_store<float>(a, cache->batch, (hipStream_t)stream)
-                         : rc::launch_qcache_store<bf16>(a, cache->batch, (hipStream_t)stream));
+  int max_rows = 0;
+  for (int b = 0; b < active->batch; ++b) max_rows = std::max(max_rows, active->offsets_host[b + 1] - active->offsets_host[b]);
+  // (every token of every chain: an ascending list has them in order)
+  if (active->offsets_host[active->batch] == (long long)cache->tokens * cache->batch) a.idx = nullptr;
+  RC_HIP(dtype == RC_F32 ? rc::launch_qcache_store<float>(a, cache->batch, max_rows, (hipStream_t)stream)
+                         : rc::launch_qcache_store<bf16>(a, cache->batch, max_rows, (hipStream_t)stream));
   return RC_OK;
 }
 

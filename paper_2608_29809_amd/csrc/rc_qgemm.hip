@@ -181,11 +181,11 @@ __global__ __launch_bounds__(64 * KG) void qgemm_split_kernel(QGemmArgs g) {
 // the epilogues.  256 x 256 tiles (64 x 128 per wave, 125 bytes per clock) have
 // one workgroup per CU: 111 and 133 us, and 128 instead of 105 at 16384 x 1152 x
 // 4608.  723 x 1152 x 4608 (64 x 64 tiles, KG = 4): 16 us, 34 with 128 x 128.
-template <int FM, int FN, int WGM, int WGN, int KG, int S, bool GELU, typename OUT>
+template <int FM, int FN, int WGM, int WGN, int KG, int S, int EPI, typename OUT>
 __global__ __launch_bounds__(64 * WGM * WGN * KG, 2) void qgemm_kernel(QGemmArgs g) {
   constexpr int NG = WGM * WGN, NW = NG * KG, BM = 16 * FM * WGM, BN = 16 * FN * WGN;
   static_assert(KG == 1 || NG == 1, "groups of one wave");
-  constexpr bool F32 = sizeof(OUT) == 4;
+  constexpr bool F32 = EPI <= QG_GELU && sizeof(OUT) == 4, GELU = EPI == QG_GELU || EPI == QG_GELU8;
   constexpr int STAGE = (BM + BN) * kQBlock, NL = STAGE / 1024 / NG, NA = BM * kQBlock / 1024 / NG;
   static_assert(STAGE % (1024 * NG) == 0 && BM * kQBlock % (1024 * NG) == 0 && kQBlock % (16 * FN) == 0, "tile");
   constexpr int NB = (BN + kQBlock - 1) / kQBlock;
@@ -342,17 +342,58 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, 2) void qgemm_kernel(QGemmArgs
   // columns and the code is a short loop (run once, each instruction of it is
   // fetched from memory).
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  if constexpr (EPI == QG_GELU8) {
+    // 64 rows at a time, whole blocks of 128 columns: sixteen lanes a row
+    static_assert(EPI != QG_GELU8 || (KG == 1 && BN == kQBlock && FM == 4 && 64 * (BN + 4) * 4 <= RING), "blocks of 128 columns");
+    float *tile = (float *)lds;
+    const int c8 = (tid & 15) * 8;
+    float bias[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias[e] = g.bias[n0 + c8 + e];
+#pragma nounroll
+    for (int pass = 0; pass < WGM; ++pass) {
+      if (wm == pass)
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) *(f32x4 *)(tile + (i * 16 + l16) * (BN + 4) + wn * WN + j * 16 + lq * 4) = acc[i][j];
+      __syncthreads();
+#pragma nounroll
+      for (int r = tid >> 4; r < 64; r += 4 * NW) {
+        float v[8], m = 0.0f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 x = *(const f32x4 *)(tile + r * (BN + 4) + c8 + 4 * h);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[4 * h + e] = gelu_tanh(x[e] + bias[4 * h + e]);
+            m = fmaxf(m, q_magnitude(v[4 * h + e]));
+          }
+        }
+        const int ex = q_exponent(row16_max(m)), row = m0 + pass * 64 + r;
+        if (row >= g.M) continue;
+        *(u32x2 *)((uint8_t *)g.out + row * g.ldo + n0 + c8) = u32x2{q_pack4(v, q_inverse(ex)), q_pack4(v + 4, q_inverse(ex))};
+        if ((tid & 15) == 0) g.out_scales[(size_t)(n0 / kQBlock) * g.out_scale_ld + row] = (uint8_t)ex;
+      }
+      __syncthreads();
+    }
+    return;
+  }
   // Rows that are a multiple of 16 bytes apart: eight columns a lane.  Others:
   // one column a lane, so that a store covers whole lines all the same.
   float *res = (float *)lds;
   constexpr int ROWS = KG == 1 ? 16 : BM, COLS = KG == 1 ? WN : BN, WHO = KG == 1 ? 64 : 64 * KG;
   const int who = KG == 1 ? lane : tid, col0 = n0 + (KG == 1 ? wn * WN : 0);
   OUT *out = (OUT *)g.out;
-  const bool vec = (g.ldo & 7) == 0;
+  const bool vec = EPI == QG_RESID || (g.ldo & 7) == 0;
   const int c8 = vec ? who % (COLS / 8) * 8 : who % COLS, col = col0 + c8;
   float bias[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) bias[e] = g.bias ? g.bias[min(col + e, g.N - 1)] : 0.0f;
+  float gate[8];
+  if (EPI == QG_RESID)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) gate[e] = g.gate[min(col + e, g.N - 1)] + g.gate2[min(col + e, g.N - 1)];
   // rows row0 .. + ROWS of the result from `tile`, the groups' sums joined in order
   auto put = [&](const float *tile, int row0) {
     if (vec) {
@@ -375,6 +416,19 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, 2) void qgemm_kernel(QGemmArgs
           }
         }
         if (row0 + r >= g.M) break;
+        if constexpr (EPI == QG_RESID) {
+          if (col >= g.N) break;
+          f32x4 *x = (f32x4 *)(g.X + (size_t)(row0 + r) * g.N + col);
+          const f32x4 x0 = x[0], x1 = x[1];
+          const int pk = g.packed[row0 + r];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = (e < 4 ? x0[e] : x1[e - 4]) + gate[e] * v[e];
+          x[0] = f32x4{v[0], v[1], v[2], v[3]};
+          x[1] = f32x4{v[4], v[5], v[6], v[7]};
+          *(bf16x8 *)(g.hslot + row_chain(pk) * g.chain_stride + (size_t)row_token(pk) * g.N + col) =
+              bf16x8{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3], (bf16)v[4], (bf16)v[5], (bf16)v[6], (bf16)v[7]};
+          continue;
+        }
         OUT *o = out + (row0 + r) * g.ldo + col;
         if (col + 8 <= g.N) {
           if constexpr (F32) {
@@ -422,21 +476,26 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, 2) void qgemm_kernel(QGemmArgs
   }
 }
 
-template <bool GELU, typename OUT> static void launch_qg(const QGemmArgs &a, const QGemmPlan &p, hipStream_t s) {
+template <int EPI, typename OUT> static hipError_t launch_qg(const QGemmArgs &a, const QGemmPlan &p, hipStream_t s) {
   const unsigned tiles = (unsigned)(((long long)a.M + p.bm - 1) / p.bm * ((a.N + p.bn - 1) / p.bn));
-#define RC_QG_SPLIT(FM, FN, KG) rc_launch(qgemm_split_kernel<FM, FN, KG, GELU, OUT>, dim3(tiles), dim3(64 * KG), 0, s, a)
+#define RC_QG_SPLIT(FM, FN, KG) \
+  return rc_launch(qgemm_split_kernel<FM, FN, KG, EPI == QG_GELU, OUT>, dim3(tiles), dim3(64 * KG), 0, s, a)
 #define RC_QG(FM, FN, WGM, WGN, KG, S) \
-  rc_launch(qgemm_kernel<FM, FN, WGM, WGN, KG, S, GELU, OUT>, dim3(tiles), dim3(64 * WGM * WGN * KG), 0, s, a)
-  switch (p.bm * 1000 + p.bn) {
-    case 16016: (void)RC_QG_SPLIT(1, 1, 8); break;
-    case 32032: (void)RC_QG_SPLIT(2, 2, 8); break;
-    case 64032: (void)RC_QG(4, 2, 1, 1, 4, 3); break;
-    case 64064: (void)RC_QG(4, 4, 1, 1, 4, 2); break;
-    case 64128: (void)RC_QG(4, 2, 1, 4, 1, 3); break;
-    case 128128: (void)RC_QG(4, 4, 2, 2, 1, 2); break;
+  return rc_launch(qgemm_kernel<FM, FN, WGM, WGN, KG, S, EPI, OUT>, dim3(tiles), dim3(64 * WGM * WGN * KG), 0, s, a)
+  const int tile = p.bm * 1000 + p.bn;
+  if constexpr (EPI <= QG_GELU) {
+    if (tile == 16016) RC_QG_SPLIT(1, 1, 8);
+    if (tile == 32032) RC_QG_SPLIT(2, 2, 8);
   }
+  if constexpr (EPI != QG_GELU8) {
+    if (tile == 64032) RC_QG(4, 2, 1, 1, 4, 3);
+    if (tile == 64064) RC_QG(4, 4, 1, 1, 4, 2);
+  }
+  if (tile == 64128) RC_QG(4, 2, 1, 4, 1, 3);
+  if (tile == 128128) RC_QG(4, 4, 2, 2, 1, 2);
 #undef RC_QG
 #undef RC_QG_SPLIT
+  return hipErrorInvalidValue;
 }
 
 // The tile with the least estimated time: 5 us of ends, and for each step of K
@@ -445,7 +504,7 @@ template <bool GELU, typename OUT> static void launch_qg(const QGemmArgs &a, con
 // float32 6.6 (32 x 32; 64 x 32 8.1), 154 x 1152 x 4608 11.6 (64 x 32; 32 x 32
 // 13.0), 723 x 1152 x 4608 16.0 (64 x 64; 64 x 32 21), 723 x 4608 x 1152 14.0 (64 x
 // 128; 128 x 128 14.9, 64 x 64 26), 2458 x 4608 x 1152 30 (128 x 128; 64 x 128 35).
-QGemmPlan plan_qgemm(int M, int N, int K) {
+QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi) {
   struct Tile { int bm, bn, kg; double fixed, per; };  // us a step, and a step per workgroup of a CU
   static constexpr Tile tiles[] = {{16, 16, 8, 0.0, 0.6}, {32, 32, 8, 0.0, 1.2}, {64, 32, 4, 0.0, 0.8},
                                    {64, 64, 4, 0.0, 1.25}, {64, 128, 1, 0.15, 0.5}, {128, 128, 1, 0.3, 0.8}};
@@ -453,6 +512,7 @@ QGemmPlan plan_qgemm(int M, int N, int K) {
   QGemmPlan best{128, 128};
   double best_us = 1e30;
   for (const Tile &t : tiles) {
+    if ((epi == QG_GELU8 && t.bn != kQBlock) || (epi == QG_RESID && t.bm < 64)) continue;  // (tiles that have the epilogue)
     const double wgs = std::ceil((double)M / t.bm) * std::ceil((double)N / t.bn) / 256;
     const double load = t.kg > 1 ? std::ceil(wgs) : std::max(wgs, 1.0), steps = (blocks + t.kg - 1) / t.kg;
     const double us = 5.0 + steps * (t.fixed + t.per * load);
@@ -464,12 +524,20 @@ QGemmPlan plan_qgemm(int M, int N, int K) {
   return best;
 }
 
-hipError_t launch_qgemm(const QGemmArgs &a, const QGemmPlan &p, bool gelu, bool f32_out, hipStream_t s) {
+hipError_t launch_qgemm(const QGemmArgs &a, const QGemmPlan &p, QGemmEpi epi, bool f32_out, hipStream_t s) {
   if (a.M <= 0) return hipSuccess;
-  if (a.K > kQMaxBlocks * kQBlock || a.K % 16) return hipErrorInvalidValue;
-  if (f32_out) gelu ? launch_qg<true, float>(a, p, s) : launch_qg<false, float>(a, p, s);
-  else gelu ? launch_qg<true, bf16>(a, p, s) : launch_qg<false, bf16>(a, p, s);
-  return hipGetLastError();
+  if (a.K > kQMaxCols || a.K % 16) return hipErrorInvalidValue;
+  hipError_t e = hipErrorInvalidValue;
+  if (epi == QG_GELU8) {
+    if (a.N % kQBlock == 0 && a.bias) e = launch_qg<QG_GELU8, bf16>(a, p, s);
+  } else if (epi == QG_RESID) {
+    if (a.N % 8 == 0) e = launch_qg<QG_RESID, bf16>(a, p, s);
+  } else if (epi == QG_GELU) {
+    e = f32_out ? launch_qg<QG_GELU, float>(a, p, s) : launch_qg<QG_GELU, bf16>(a, p, s);
+  } else {
+    e = f32_out ? launch_qg<QG_STORE, float>(a, p, s) : launch_qg<QG_STORE, bf16>(a, p, s);
+  }
+  return e != hipSuccess ? e : hipGetLastError();
 }
 
 }  // namespace rc

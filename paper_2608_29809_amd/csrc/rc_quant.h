@@ -31,27 +31,25 @@ struct QuantArgs {
 };
 template <typename T> hipError_t launch_quantize(const QuantArgs &a, int block_rows, hipStream_t s);
 
-// A step's rows between two 8-bit products, one pass over each: the product of
-// the MLP's second matrix joins the residual stream and the cached hidden
-// state (y set), and the LayerNorm + modulation for the next product leaves in
-// 8 bits (q set).
+// LayerNorm + modulation of a step's rows, into 8 bits.
 struct NormQuantArgs {
-  float *X;                 // [rows][C]
+  const float *X;           // [rows][C]
   int rows, C;
-  const float *y;           // [rows][C] or null; X += (gate + gate2) (y + bias)
-  const float *bias, *gate, *gate2;
-  const int *packed;        // packed (chain << 16) | token per row
-  bf16 *hslot;              // H of chain 0's slot
-  long long chain_stride;   // elements
   const float *sst, *t0;    // shift and scale: rows shift_row and shift_row + 1 of sst + t0
   int shift_row;
   float eps;
-  uint8_t *q;               // [rows][C] or null
+  uint8_t *q;               // [rows][C]
   uint8_t *scales;          // [C / 128][scale_ld]
   int scale_ld;
 };
 hipError_t launch_norm_quantize(const NormQuantArgs &a, hipStream_t s);
 
+enum QGemmEpi {
+  QG_STORE = 0,  // out = acc + bias, bfloat16 or float32
+  QG_GELU = 1,   // out = gelu_tanh(acc + bias), bfloat16 or float32
+  QG_GELU8 = 2,  // the same in 8 bits with a scale for each row and 128 columns (N a multiple of 128)
+  QG_RESID = 3,  // X += (gate + gate2) (acc + bias), and the new X in bfloat16 into the rows' places in hslot (N a multiple of 8)
+};
 struct QGemmArgs {
   const uint8_t *a, *w;     // [M][K], [N][K]
   const uint8_t *as, *ws;   // scales: [K blocks][as_ld], [K blocks][ws_ld]
@@ -59,12 +57,21 @@ struct QGemmArgs {
   int as_ld, ws_ld;
   int M, N, K;
   const float *bias;        // [N] or null
-  void *out;
+  void *out;                // QG_GELU8: e4m3
   long long ldo;            // elements
+  // QG_GELU8
+  uint8_t *out_scales;      // [N / 128][out_scale_ld]
+  int out_scale_ld;
+  // QG_RESID
+  float *X;                 // [M][N]
+  const float *gate, *gate2;
+  const int *packed;        // (chain << 16) | token per row
+  bf16 *hslot;              // H of chain 0's slot
+  long long chain_stride;   // elements
 };
 struct QGemmPlan { int bm, bn; };  // workgroup tile
-QGemmPlan plan_qgemm(int M, int N, int K);
-hipError_t launch_qgemm(const QGemmArgs &a, const QGemmPlan &p, bool gelu, bool f32_out, hipStream_t s);
+QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi);
+hipError_t launch_qgemm(const QGemmArgs &a, const QGemmPlan &p, QGemmEpi epi, bool f32_out, hipStream_t s);
 
 struct QCacheArgs {
   uint8_t *data;            // [heads][tokens / 64][2][64][72] per chain: keys, then values, of a block
@@ -90,7 +97,7 @@ struct QStoreArgs {
   const void *k, *v;        // [rows][heads * 72]
   long long ld;             // elements
 };
-template <typename T> hipError_t launch_qcache_store(const QStoreArgs &a, int chains, hipStream_t s);
+template <typename T> hipError_t launch_qcache_store(const QStoreArgs &a, int chains, int max_rows, hipStream_t s);
 
 struct QAttnArgs {
   QCacheArgs c;
@@ -140,6 +147,14 @@ __device__ __forceinline__ uint32_t q_pack4(const float *x, float inv) {
   r = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
   return (uint32_t)r;
 }
+// Maximum over the 16 lanes of a DPP row.
+__device__ __forceinline__ float row16_max(float v) {
+  v = fmaxf(v, dpp_mov<0xB1>(v));
+  v = fmaxf(v, dpp_mov<0x4E>(v));
+  v = fmaxf(v, dpp_mov<0x141>(v));
+  return fmaxf(v, dpp_mov<0x140>(v));
+}
+
 typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

@@ -21,14 +21,6 @@ template <> __device__ __forceinline__ void q_load8<bf16>(const bf16 *p, float *
   for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
 }
 
-// Maximum over the 16 lanes of a DPP row.
-__device__ __forceinline__ float row16_max(float v) {
-  v = fmaxf(v, dpp_mov<0xB1>(v));
-  v = fmaxf(v, dpp_mov<0x4E>(v));
-  v = fmaxf(v, dpp_mov<0x141>(v));
-  return fmaxf(v, dpp_mov<0x140>(v));
-}
-
 // A scale for each row and 128 columns: sixteen lanes take a block, eight
 // columns each.
 template <typename T> __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a, int cb) {
@@ -97,7 +89,7 @@ __global__ __launch_bounds__(256) void norm_quantize_kernel(NormQuantArgs a) {
   __shared__ float red[4];
   const int r = blockIdx.x, t = threadIdx.x, C4 = a.C >> 2;
   constexpr int MAXV = 2;  // C <= 4 * 256 * MAXV
-  float *X = a.X + (size_t)r * a.C;
+  const float *X = a.X + (size_t)r * a.C;
   const f32x4 zero4 = {0.0f, 0.0f, 0.0f, 0.0f};
   f32x4 x[MAXV], shift[MAXV], scale[MAXV];
   const float *sh = a.sst + (size_t)a.shift_row * a.C, *tsh = a.t0 + (size_t)a.shift_row * a.C;
@@ -105,26 +97,12 @@ __global__ __launch_bounds__(256) void norm_quantize_kernel(NormQuantArgs a) {
 #pragma unroll
   for (int i = 0; i < MAXV; ++i) {
     const int n = (t + 256 * i) * 4;
-    x[i] = shift[i] = scale[i] = zero4;
-    if (n >= a.C) continue;
-    x[i] = *(const f32x4 *)(X + n);
-    if (a.q) {
-      shift[i] = *(const f32x4 *)(sh + n) + *(const f32x4 *)(tsh + n);
-      scale[i] = *(const f32x4 *)(sh + a.C + n) + *(const f32x4 *)(tsh + a.C + n);
-    }
-    if (a.y) {
-      const f32x4 y = *(const f32x4 *)(a.y + (size_t)r * a.C + n) + *(const f32x4 *)(a.bias + n);
-      const f32x4 g = *(const f32x4 *)(a.gate + n) + *(const f32x4 *)(a.gate2 + n);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] += g[e] * y[e];
-      *(f32x4 *)(X + n) = x[i];
-      const int pk = a.packed[r];
-      *(bf16x4 *)(a.hslot + row_chain(pk) * a.chain_stride + (size_t)row_token(pk) * a.C + n) =
-          bf16x4{(bf16)x[i][0], (bf16)x[i][1], (bf16)x[i][2], (bf16)x[i][3]};
-    }
+    const bool in = n < a.C;
+    x[i] = in ? *(const f32x4 *)(X + n) : zero4;
+    shift[i] = in ? *(const f32x4 *)(sh + n) + *(const f32x4 *)(tsh + n) : zero4;
+    scale[i] = in ? *(const f32x4 *)(sh + a.C + n) + *(const f32x4 *)(tsh + a.C + n) : zero4;
     s += (x[i][0] + x[i][1]) + (x[i][2] + x[i][3]);
   }
-  if (!a.q) return;
   const float mean = block4_sum(s, red) / a.C;
   float d2 = 0.0f;
 #pragma unroll
@@ -160,76 +138,100 @@ hipError_t launch_norm_quantize(const NormQuantArgs &a, hipStream_t s) {
 
 // ------------------------------------------------------------------ cache store
 
-// First position in [lo, hi) of an ascending list whose entry is >= key: the
-// wave probes 64 places at a time.
-__device__ __forceinline__ int wave_lower_bound(const int *idx, int lo, int hi, int key) {
-  const int lane = threadIdx.x & 63;
-  while (lo < hi) {
-    const int step = (hi - lo + 63) >> 6;  // places lo, lo + step, ...
-    const int at = lo + lane * step;
-    const unsigned long long less = __ballot(at < hi && idx[min(at, hi - 1)] < key);
-    const int n = __popcll(less);  // (ascending: the lanes below are the first n)
-    if (n == 0) return lo;
-    const int last = lo + (n - 1) * step;
-    lo = last + 1;
-    hi = min(hi, last + step);
-  }
-  return lo;
-}
-
-// One workgroup per chain, block of 64 tokens, head, and keys or values.  The
-// block's fresh rows take the places of their tokens, the others keep their
-// values; the scale is that of the merged block.
-template <typename T> __global__ __launch_bounds__(192) void qcache_store_kernel(QStoreArgs a) {
+// A workgroup takes one head's keys or values in the blocks of 64 tokens whose
+// first active row is among its `chunk` rows of the list.  A block's fresh rows
+// take the places of their tokens, the others keep their values; the scale is
+// that of the merged tile.  Bound by latency for a region (the list, then the
+// values and the old tile), by its bytes for every token of a dense step (idx
+// null: workgroup x takes block x).
+template <typename T> __global__ __launch_bounds__(192) void qcache_store_kernel(QStoreArgs a, int chunk) {
   constexpr int CPR = kHeadDim / 8;  // chunks of eight values per token
   __shared__ int row_of[kQTokens];
   __shared__ float red[3];
-  const int tid = threadIdx.x, blk = blockIdx.x, head = blockIdx.y >> 1, which = blockIdx.y & 1, b = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 63, head = blockIdx.y >> 1, which = blockIdx.y & 1, b = blockIdx.z;
   const int2 rr = chain_rows(a.rows, b);
+  const int blocks = a.c.tokens / kQTokens, r0 = rr.x + (int)blockIdx.x * chunk;
+  // list entries r0 - 1 + lane and r0 + 63 + lane (the same in every wave); the
+  // blocks that begin here (its first lanes of them)
+  int tok0 = -1, tok1 = -1;
+  unsigned long long first = 1;
   if (a.idx) {
-    const int lo = wave_lower_bound(a.idx, rr.x, rr.y, blk * kQTokens);
-    const int hi = wave_lower_bound(a.idx, lo, min(rr.y, lo + kQTokens), (blk + 1) * kQTokens);
-    if (lo >= hi) return;
-    if (tid < kQTokens) row_of[tid] = -1;
-    __syncthreads();
-    if (tid < hi - lo) row_of[a.idx[lo + tid] & (kQTokens - 1)] = lo + tid;
-  } else if (tid < kQTokens) {
-    row_of[tid] = rr.x + blk * kQTokens + tid;
+    if (r0 >= rr.y) return;
+    const int at = r0 - 1 + lane;
+    if (at >= rr.x && at < rr.y) tok0 = a.idx[at];
+    if (at + 64 < rr.y) tok1 = a.idx[at + 64];
+    const int before = __shfl_up(tok0, 1, 64);
+    first = __ballot(lane >= 1 && lane <= chunk && tok0 >= 0 && (before < 0 || (before >> 6) != (tok0 >> 6)));
   }
-  __syncthreads();
-  const size_t tile = ((size_t)head * (a.c.tokens / kQTokens) + blk) * 2 + which;
-  uint8_t *data = a.c.data + b * a.c.chain_stride + tile * kQTileBytes;
-  uint8_t *scale = a.c.scales + b * a.c.scale_chain_stride + tile;
-  const T *src = (const T *)(which ? a.v : a.k) + head * kHeadDim;
-  const float old = q_factor(*scale);
-  float v[3][8], m = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const int c = tid + i * 192, tok = c / CPR, d = (c - tok * CPR) * 8, r = row_of[tok];
-    if (r >= 0) {
-      q_load8<T>(src + r * a.ld + d, v[i]);
-    } else {
-      q_f32x8(*(const u32x2 *)(data + c * 8), old, v[i]);
+  for (; first; first &= first - 1) {
+    const int pos = __ffsll((long long)first) - 1;
+    const int blk = a.idx ? __shfl(tok0, pos, 64) >> 6 : (int)blockIdx.x;
+    if (blk >= blocks) break;  // (an invalid list: nothing is written)
+    // rows of the block (contiguous, from any_row on; all of it: a dense step's)
+    const int any_row = a.idx ? r0 - 1 + pos : rr.x + blk * kQTokens;
+    const bool full = !a.idx || __popcll(__ballot(tok0 >= 0 && tok0 >> 6 == blk && lane >= pos)) +
+                                        __popcll(__ballot(tok1 >= 0 && tok1 >> 6 == blk)) == kQTokens;
+    __syncthreads();           // the block before is done with row_of and red
+    if (tid < 64) {
+      row_of[lane] = a.idx ? -1 : rr.x + blk * kQTokens + lane;
+      __builtin_amdgcn_wave_barrier();
+      if (a.idx) {
+        if (lane >= pos && tok0 >= 0 && tok0 >> 6 == blk) row_of[tok0 & 63] = r0 - 1 + lane;
+        if (tok1 >= 0 && tok1 >> 6 == blk) row_of[tok1 & 63] = r0 + 63 + lane;
+      }
     }
+    __syncthreads();
+    const size_t tile = ((size_t)head * blocks + blk) * 2 + which;
+    uint8_t *data = a.c.data + b * a.c.chain_stride + tile * kQTileBytes;
+    uint8_t *scale = a.c.scales + b * a.c.scale_chain_stride + tile;
+    const T *src = (const T *)(which ? a.v : a.k) + head * kHeadDim;
+    // every load before the first use: fresh rows (kept tokens read the block's
+    // first one), and the old tile unless every token is fresh
+    float v[3][8], old = 0.0f, m = 0.0f;
+    u32x2 kept[3];
+    int r[3];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) m = fmaxf(m, q_magnitude(v[i][k]));
+    for (int i = 0; i < 3; ++i) {
+      const int c = tid + i * 192, tok = c / CPR, d = (c - tok * CPR) * 8;
+      r[i] = row_of[tok];
+      kept[i] = u32x2{0u, 0u};
+      if (!full) kept[i] = *(const u32x2 *)(data + c * 8);
+      q_load8<T>(src + (r[i] >= 0 ? r[i] : any_row) * a.ld + d, v[i]);
+    }
+    if (!full) old = q_factor(*scale);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      float w[8];
+      q_f32x8(kept[i], old, w);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        v[i][k] = r[i] >= 0 ? v[i][k] : w[k];
+        m = fmaxf(m, q_magnitude(v[i][k]));
+      }
+    }
+    m = wave_max(m);
+    if (lane == 0) red[tid >> 6] = m;
+    __syncthreads();
+    const int e = q_exponent(fmaxf(fmaxf(red[0], red[1]), red[2]));
+    const float inv = q_inverse(e);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) *(u32x2 *)(data + (tid + i * 192) * 8) = u32x2{q_pack4(v[i], inv), q_pack4(v[i] + 4, inv)};
+    if (tid == 0) *scale = (uint8_t)e;
   }
-  m = wave_max(m);
-  if ((tid & 63) == 0) red[tid >> 6] = m;
-  __syncthreads();
-  const int e = q_exponent(fmaxf(fmaxf(red[0], red[1]), red[2]));
-  const float inv = q_inverse(e);
-#pragma unroll
-  for (int i = 0; i < 3; ++i) *(u32x2 *)(data + (tid + i * 192) * 8) = u32x2{q_pack4(v[i], inv), q_pack4(v[i] + 4, inv)};
-  if (tid == 0) *scale = (uint8_t)e;
 }
 
-template <typename T> hipError_t launch_qcache_store(const QStoreArgs &a, int chains, hipStream_t s) {
-  if (chains <= 0) return hipSuccess;
-  rc_launch(qcache_store_kernel<T>, dim3(a.c.tokens / kQTokens, 2 * a.c.heads, chains), dim3(192), 0, s, a);
+// Rows per workgroup: as few (down to 1, at most 32) as leave no more workgroups
+// than run at once, about 1536, so that scattered tokens, each with a block of
+// its own, are spread too.
+template <typename T> hipError_t launch_qcache_store(const QStoreArgs &a, int chains, int max_rows, hipStream_t s) {
+  if (chains <= 0 || max_rows <= 0) return hipSuccess;
+  int chunk = 1;
+  while (chunk < 32 && (long long)(max_rows + chunk - 1) / chunk * 2 * a.c.heads * chains > 1536) chunk *= 2;
+  const int x = a.idx ? (max_rows + chunk - 1) / chunk : a.c.tokens / kQTokens;
+  rc_launch(qcache_store_kernel<T>, dim3(x, 2 * a.c.heads, chains), dim3(192), 0, s, a, chunk);
   return hipGetLastError();
 }
-template hipError_t launch_qcache_store<bf16>(const QStoreArgs &, int, hipStream_t);
-template hipError_t launch_qcache_store<float>(const QStoreArgs &, int, hipStream_t);
+template hipError_t launch_qcache_store<bf16>(const QStoreArgs &, int, int, hipStream_t);
+template hipError_t launch_qcache_store<float>(const QStoreArgs &, int, int, hipStream_t);
 
 }  // namespace rc

@@ -42,7 +42,7 @@ def block(lw, X, mod, tk, tv, K, V, heads, w8):
     X = X + g1 * (o.reshape(-1, C) @ np.asarray(lw["proj_w"], np.float64).T + lw["proj_b"])
     X, _ = O.cross_and_mlp(lw, X, (sh1, sc1, g1, sh2, sc2, np.zeros_like(g2)), tk, tv, heads, None, np.float64)
     f = O.gelu_tanh(linear(lw, "fc1", O.modulate(O.layer_norm(X), sh2, sc2), w8) + lw["fc1_b"])
-    return X + g2 * (linear(lw, "fc2", bf16(f) if w8 else f, w8) + lw["fc2_b"]), qkv[:, C:2 * C], qkv[:, 2 * C:]
+    return X + g2 * (linear(lw, "fc2", f, w8) + lw["fc2_b"]), qkv[:, C:2 * C], qkv[:, 2 * C:]
 
 
 def slot_values(cache, t, l):

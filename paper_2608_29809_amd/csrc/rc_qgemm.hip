@@ -431,11 +431,13 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, 2) void qgemm_kernel(QGemmArgs
         }
         OUT *o = out + (row0 + r) * g.ldo + col;
         if (col + 8 <= g.N) {
+          // (past the L2, which the operands need: 134 instead of 165 us for 16384 x 4608 x 1152 with GELU)
           if constexpr (F32) {
-            *(f32x4 *)o = f32x4{v[0], v[1], v[2], v[3]};
-            *(f32x4 *)(o + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, (f32x4 *)o);
+            __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, (f32x4 *)(o + 4));
           } else {
-            *(bf16x8 *)o = bf16x8{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3], (bf16)v[4], (bf16)v[5], (bf16)v[6], (bf16)v[7]};
+            __builtin_nontemporal_store(
+                bf16x8{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3], (bf16)v[4], (bf16)v[5], (bf16)v[6], (bf16)v[7]}, (bf16x8 *)o);
           }
         } else {
 #pragma unroll

@@ -367,10 +367,12 @@ rc_status rc_compact_mask(const uint8_t *mask, int32_t batch, int32_t tokens, in
  * 8-bit floating-point numbers (e4m3: 4 exponent bits, 3 of mantissa, largest
  * value 448, no infinity) in blocks that share a scale.  A scale is a power of
  * two held as one byte e, 2^(e - 127), 1 <= e <= 254; a block that is all
- * zeros may have any byte, so zeroed memory is a valid block of zeros.  The
+ * zeros may have 0 too, so zeroed memory is a valid block of zeros.  The
  * calls that write blocks choose the least e >= 1 with which the block's
  * largest finite magnitude is at most 448 units, and round to nearest even;
- * values that are not finite become NaN and do not count for the scale.
+ * values that are not finite become NaN and do not count for the scale.  (A
+ * float32 of more than 1.9375 * 2^127 becomes 2^128, an infinity to the calls
+ * that read it.)
  * These calls take no context.  They follow the conventions above: buffers
  * belong to the caller, work goes to `stream` of the current device, nothing
  * synchronises, nothing is kept between calls, and each may be captured into a
@@ -381,7 +383,8 @@ rc_status rc_compact_mask(const uint8_t *mask, int32_t batch, int32_t tokens, in
  * lower edge are smaller where rows or cols end inside one. */
 typedef struct {
   void *data;          /* device e4m3, rows `ld` bytes apart */
-  uint8_t *scales;     /* device: entry (column block j, row block i) is scales[j*scale_ld + i] */
+  uint8_t *scales;     /* device: entry (column block j, row block i) is scales[j*scale_ld + i];
+                          read up to a multiple of 16 row blocks, whatever stands there */
   int64_t ld;          /* a multiple of 16, >= cols */
   int32_t rows, cols;  /* cols a multiple of 16, at most 65536 */
   int32_t scale_ld;    /* a multiple of 16, >= row blocks */
@@ -397,7 +400,8 @@ rc_status rc_quantize(const void *x, int32_t dtype, int64_t ldx, const rc_qmat *
  * if 0.  bias: device float32 [w->rows], or NULL.  out: device, rc_dtype
  * out_dtype, rows ldo >= w->rows elements apart.  Sums are float32; a bfloat16
  * result is rounded once, and its sums of 128 products are exact to about 17
- * bits; a float32 result has float32's precision throughout. */
+ * bits; a float32 result has float32's precision throughout.  At most 2^32
+ * results (RC_ERR_SHAPE). */
 rc_status rc_qgemm(const rc_qmat *a, const rc_qmat *w, const float *bias, int32_t gelu, void *out,
                    int32_t out_dtype, int64_t ldo, void *stream);
 
@@ -434,7 +438,9 @@ rc_status rc_qcache_store(const rc_qcache *cache, const rc_active_set *active, c
  * device bfloat16, heads side by side, rows ldq / ldo elements apart
  * (multiples of 8).  scratch: 16-byte aligned device memory of
  * rc_qcache_attention_scratch_bytes(cache, rows) bytes (may be NULL where that
- * is 0); calls that may overlap in time need scratch of their own. */
+ * is 0); calls that may overlap in time need scratch of their own.  At most
+ * 2^24 rows and 2^23 workgroups (a head's 16 to 256 rows of a chain each, and
+ * of more than 16 chains the most rows count for every one): RC_ERR_SHAPE. */
 size_t rc_qcache_attention_scratch_bytes(const rc_qcache *cache, const rc_active_set *rows);
 rc_status rc_qcache_attention(const rc_qcache *cache, const rc_active_set *rows, const int32_t *key_len,
                               const void *q, int64_t ldq, float scale, void *out, int64_t ldo, void *scratch,

@@ -9,6 +9,7 @@
 #include <cstdio>
 #include <cstring>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -564,14 +565,12 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
     return timed(c, cls, s, [&] { return rc::launch_qgemm(g, rc::plan_qgemm(g.M, g.N, g.K, epi), epi, false, s); });
   };
   rc::ChainRows q_rows{};
-  rc::QAttnPlan q_plan{1, 1};
+  rc::QAttnPlan q_plan{};
   if (quant) {
-    std::vector<int> offs(B + 1);
-    for (int b = 0; b <= B; ++b) offs[b] = dense ? b * N : act->offsets_host[b];
     q_rows.offsets = offsets_dev;
     q_rows.n_arg = std::min(B, rc::kQArgChains);
-    for (int b = 0; b <= q_rows.n_arg; ++b) q_rows.arg[b] = offs[b];
-    q_plan = rc::plan_qattention(offs.data(), B, H, N);
+    for (int b = 0; b <= q_rows.n_arg; ++b) q_rows.arg[b] = dense ? b * N : act->offsets_host[b];
+    q_plan = rc::plan_qattention(dense ? nullptr : act->offsets_host, B, H, N);
   }
 
   PipeJoin pipe_join{c, s};
@@ -647,7 +646,7 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
       a.splits = q_plan.splits; a.total_rows = R;
       a.part = (float *)(qws + qw.part);
       a.ml = a.part + (q_plan.splits > 1 ? (size_t)q_plan.splits * R * C : 0);
-      RC_TRY(timed(c, RC_KC_ATTN_SELF, s, [&] { return rc::launch_qattention(a, B, max_rb, q_plan.qh, s); }));
+      RC_TRY(timed(c, RC_KC_ATTN_SELF, s, [&] { return rc::launch_qattention(a, B, q_plan, s); }));
       if (a.splits > 1)
         RC_TRY(timed(c, RC_KC_ATTN_COMBINE, s, [&] { return rc::launch_qattention_combine(a, s); }));
     }
@@ -986,9 +985,7 @@ rc::ChainRows chain_rows_args(const rc_active_set *a) {
 
 constexpr int kMaxQRows = 1 << 24;  // query rows of one attention call
 
-rc::QAttnPlan qattention_plan(const rc_qcache *c, const rc_active_set *rows, int *max_rows) {
-  *max_rows = 0;
-  for (int b = 0; b < rows->batch; ++b) *max_rows = std::max(*max_rows, rows->offsets_host[b + 1] - rows->offsets_host[b]);
+rc::QAttnPlan qattention_plan(const rc_qcache *c, const rc_active_set *rows) {
   return rc::plan_qattention(rows->offsets_host, rows->batch, c->heads, c->tokens);
 }
 
@@ -1372,7 +1369,11 @@ rc_status rc_set_quant_weights(rc_ctx *c, const rc_quant_layer *layers) {
     }
     RC_CHECK(aligned16(c->layers[l].sst), RC_ERR_ALIGN, "layer %d: 8-bit products need a 16-byte aligned modulation table", l);
   }
-  c->quant.assign(layers, layers + c->L);
+  try {
+    c->quant.assign(layers, layers + c->L);
+  } catch (const std::bad_alloc &) {
+    RC_CHECK(false, RC_ERR_CAPACITY, "no host memory for %d layers", c->L);
+  }
   return RC_OK;
 }
 
@@ -1385,6 +1386,8 @@ rc_status rc_build_cache_quant(rc_ctx *c, const rc_cache_view *cache, int32_t st
   RC_TRY(check_io(c, io));
   RC_TRY(check_guided(io, cache->batch, nullptr));
   RC_CHECK((long)cache->batch * c->N <= kMaxQRows, RC_ERR_SHAPE, "batch too large");
+  RC_CHECK(rc::plan_qattention(nullptr, cache->batch, c->H, c->N).workgroups <= rc::kQMaxWorkgroups, RC_ERR_SHAPE,
+           "too many chains and tokens for one step");
   RC_CHECK(device_present(), RC_ERR_NO_DEVICE, "no HIP device");
   return run_step<bf16>(c, cache, step, io, true, nullptr, nullptr, true, ws, ws_bytes, (hipStream_t)stream, nullptr, true);
 }
@@ -1401,6 +1404,8 @@ rc_status rc_reuse_step_quant(rc_ctx *c, const rc_cache_view *cache, int32_t ste
   RC_CHECK((flags & ~(RC_FUSE_UPDATE | RC_VALIDATE)) == 0, RC_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
   RC_CHECK(flags & RC_FUSE_UPDATE, RC_ERR_UNSUPPORTED, "an 8-bit pool is updated in place (RC_FUSE_UPDATE)");
   RC_CHECK(active->offsets_host[cache->batch] <= kMaxQRows, RC_ERR_SHAPE, "too many active tokens");
+  RC_CHECK(rc::plan_qattention(active->offsets_host, cache->batch, c->H, c->N).workgroups <= rc::kQMaxWorkgroups,
+           RC_ERR_SHAPE, "too many chains and active tokens for one step");
   if (flags & RC_VALIDATE)
     RC_CHECK(ws && aligned16(ws) && ws_bytes >= 16, RC_ERR_INVALID_ARG, "RC_VALIDATE needs the workspace");
   RC_CHECK(device_present(), RC_ERR_NO_DEVICE, "no HIP device");
@@ -1552,8 +1557,7 @@ rc_status rc_qcache_store(const rc_qcache *cache, const rc_active_set *active, c
 
 size_t rc_qcache_attention_scratch_bytes(const rc_qcache *cache, const rc_active_set *rows) {
   if (check_qcache(cache) != RC_OK || check_rows(rows, cache->batch, kMaxQRows) != RC_OK) return 0;
-  int max_rows = 0;
-  return qattention_scratch(qattention_plan(cache, rows, &max_rows), rows->offsets_host[rows->batch], cache->heads);
+  return qattention_scratch(qattention_plan(cache, rows), rows->offsets_host[rows->batch], cache->heads);
 }
 
 rc_status rc_qcache_attention(const rc_qcache *cache, const rc_active_set *rows, const int32_t *key_len, const void *q,
@@ -1567,13 +1571,14 @@ rc_status rc_qcache_attention(const rc_qcache *cache, const rc_active_set *rows,
   RC_CHECK(ldq >= C && ldo >= C, RC_ERR_SHAPE, "rows of %d values are %lld and %lld elements apart", C, (long long)ldq,
            (long long)ldo);
   RC_CHECK(ldq % 8 == 0 && ldo % 8 == 0, RC_ERR_ALIGN, "ldq and ldo must be multiples of 8");
-  RC_CHECK(std::isfinite(scale), RC_ERR_INVALID_ARG, "scale is not finite");
+  const float scale_log2 = (float)(scale * 1.4426950408889634);
+  RC_CHECK(std::isfinite(scale_log2), RC_ERR_INVALID_ARG, "scale %g is not finite, or too large", (double)scale);
   if (R == 0) return RC_OK;
   RC_CHECK(q && out, RC_ERR_INVALID_ARG, "q or out is null");
   RC_CHECK(aligned16(q) && aligned16(out), RC_ERR_ALIGN, "q/out not 16-byte aligned");
   RC_CHECK(!key_len || (reinterpret_cast<uintptr_t>(key_len) & 3u) == 0, RC_ERR_ALIGN, "key_len not 4-byte aligned");
-  int max_rows = 0;
-  const rc::QAttnPlan p = qattention_plan(cache, rows, &max_rows);
+  const rc::QAttnPlan p = qattention_plan(cache, rows);
+  RC_CHECK(p.workgroups <= rc::kQMaxWorkgroups, RC_ERR_SHAPE, "too many chains, rows and heads for one call");
   const size_t need = qattention_scratch(p, R, cache->heads);
   RC_CHECK(scratch || need == 0, RC_ERR_INVALID_ARG, "scratch is null");
   RC_CHECK(aligned16(scratch), RC_ERR_ALIGN, "scratch not 16-byte aligned");
@@ -1581,11 +1586,11 @@ rc_status rc_qcache_attention(const rc_qcache *cache, const rc_active_set *rows,
   RC_CHECK(device_present(), RC_ERR_NO_DEVICE, "no HIP device");
   rc::QAttnArgs a{};
   a.c = qcache_args(cache); a.rows = chain_rows_args(rows); a.key_len = key_len;
-  a.q = (const bf16 *)q; a.ldq = ldq; a.scale_log2 = (float)(scale * 1.4426950408889634); a.out = (bf16 *)out; a.ldo = ldo;
+  a.q = (const bf16 *)q; a.ldq = ldq; a.scale_log2 = scale_log2; a.out = (bf16 *)out; a.ldo = ldo;
   a.splits = p.splits; a.total_rows = R;
   a.part = (float *)scratch;
   a.ml = (float *)((char *)scratch + qattention_part_bytes(p, R, cache->heads));
-  RC_HIP(rc::launch_qattention(a, cache->batch, max_rows, p.qh, (hipStream_t)stream));
+  RC_HIP(rc::launch_qattention(a, cache->batch, p, (hipStream_t)stream));
   RC_HIP(rc::launch_qattention_combine(a, (hipStream_t)stream));
   return RC_OK;
 }

@@ -610,16 +610,19 @@ __global__ __launch_bounds__(64) void qattn_combine_kernel(QAttnArgs a) {
 // 16384 175 and 160; 16384 of 16384 1412 and 1204.
 QAttnPlan plan_qattention(const int *offsets, int chains, int heads, int tokens) {
   const int n_tiles = tokens / kQTokens;
-  const long rows = offsets[chains];
-  QAttnPlan best{1, 1};
+  const long long rows = offsets ? offsets[chains] : (long long)chains * tokens;
+  QAttnPlan best{1, 1, 0};
   double best_us = 1e30;
   for (int qh = 0; qh <= 2; ++qh) {
     const int bq = qh ? 128 * qh : 16;
-    long qtiles = 0, full = 0;
+    long long qtiles = 0, most = 0, full = 0;
     for (int b = 0; b < chains; ++b) {
-      qtiles += (offsets[b + 1] - offsets[b] + bq - 1) / bq;
-      full += offsets[b + 1] > offsets[b];
+      const int n = offsets ? offsets[b + 1] - offsets[b] : tokens, t = n / bq + (n % bq != 0);
+      qtiles += t;
+      most = std::max(most, (long long)t);
+      full += n > 0;
     }
+    const long long grid = (chains <= kQArgChains ? qtiles : chains * most) * heads;
     for (int sp = 1; sp <= std::min(n_tiles, kQMaxSplits) && (sp == 1 || rows * heads * sp <= kQMaxSplitRows); ++sp) {
       const double wgs = (double)qtiles * heads * sp, tiles = (n_tiles + sp - 1) / sp;
       double us = sp > 1 ? 4.0 + rows * heads * kHeadDim * 4.0 * (sp + 1) / 4e6 : 0.0;
@@ -631,27 +634,23 @@ QAttnPlan plan_qattention(const int *offsets, int chains, int heads, int tokens)
               tiles * (qh == 1 ? 1.45 * (wgs <= 256 ? 0.7 : std::ceil(wgs / 512)) : 2.3 * (wgs <= 256 ? 0.6 : std::ceil(wgs / 512)));
       if (us < best_us) {
         best_us = us;
-        best = QAttnPlan{qh, sp};
+        best = QAttnPlan{qh, sp, grid * sp};
       }
     }
   }
   return best;
 }
 
-hipError_t launch_qattention(const QAttnArgs &args, int chains, int max_rows, int qh, hipStream_t s) {
-  if (max_rows <= 0 || args.total_rows <= 0) return hipSuccess;
+hipError_t launch_qattention(const QAttnArgs &args, int chains, const QAttnPlan &p, hipStream_t s) {
+  if (p.workgroups <= 0 || args.total_rows <= 0) return hipSuccess;
+  if (p.workgroups > kQMaxWorkgroups) return hipErrorInvalidValue;
   QAttnArgs a = args;
   // (a scale of 0 becomes one that rounds away: the masks' -3.4e38 must keep its sign)
   if (std::fabs(a.scale_log2) < 1e-30f) a.scale_log2 = 1e-30f;
   a.chains = chains;
-  const int bq = qh ? 128 * qh : 16;
-  long long tiles_q = 0;
-  if (chains <= kQArgChains)
-    for (int b = 0; b < chains; ++b) tiles_q += (a.rows.arg[b + 1] - a.rows.arg[b] + bq - 1) / bq;
-  else tiles_q = (long long)chains * ((max_rows + bq - 1) / bq);
-  const dim3 grid((unsigned)(tiles_q * a.c.heads * a.splits));
-  if (qh == 0) rc_launch(qattn_few_kernel, grid, dim3(256), 0, s, a);
-  else if (qh == 2) rc_launch(qattn_kernel<2>, grid, dim3(256), 0, s, a);
+  const dim3 grid((unsigned)p.workgroups);
+  if (p.qh == 0) rc_launch(qattn_few_kernel, grid, dim3(256), 0, s, a);
+  else if (p.qh == 2) rc_launch(qattn_kernel<2>, grid, dim3(256), 0, s, a);
   else rc_launch(qattn_kernel<1>, grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }

@@ -217,8 +217,8 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, 2) void qgemm_kernel(QGemmArgs
                     : (unsigned)min(row8 + (i - NA) * NG * 8, g.N - 1 - n0) * (unsigned)g.ldw;
   char *ring = lds + grp * S * STAGE, *scales = lds + RING + grp * S * BM;
   const unsigned ring0 = lds_address(ring) + wg * 1024, scales0 = lds_address(scales);
-  // (row scales: 16 a lane, by the group's first wave; their rows are padded to 16)
-  const unsigned sc_off = (unsigned)min(lane * 16, g.as_ld - 16 - m0);
+  // (row scales: 16 a lane, by the group's first wave, up to a multiple of 16 rows)
+  const unsigned sc_off = (unsigned)min(lane * 16, (g.M - 1 - m0) & ~15);
   auto issue = [&](int slot, int i) {
     const int kb = grp + KG * i;
 #pragma unroll
@@ -479,7 +479,9 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, 2) void qgemm_kernel(QGemmArgs
 }
 
 template <int EPI, typename OUT> static hipError_t launch_qg(const QGemmArgs &a, const QGemmPlan &p, hipStream_t s) {
-  const unsigned tiles = (unsigned)(((long long)a.M + p.bm - 1) / p.bm * ((a.N + p.bn - 1) / p.bn));
+  const long long n = ((long long)a.M + p.bm - 1) / p.bm * (((long long)a.N + p.bn - 1) / p.bn);
+  if (n > 1 << 22) return hipErrorInvalidValue;  // (a grid holds fewer than 2^32 threads)
+  const unsigned tiles = (unsigned)n;
 #define RC_QG_SPLIT(FM, FN, KG) \
   return rc_launch(qgemm_split_kernel<FM, FN, KG, EPI == QG_GELU, OUT>, dim3(tiles), dim3(64 * KG), 0, s, a)
 #define RC_QG(FM, FN, WGM, WGN, KG, S) \

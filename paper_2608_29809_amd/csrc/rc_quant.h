@@ -116,9 +116,14 @@ struct QAttnArgs {
 };
 constexpr int kQMaxSplits = 16;
 constexpr long kQMaxSplitRows = 1L << 18;  // rows x heads x splits of a split plan
-struct QAttnPlan { int qh, splits; };  // qh: 32-query halves per wave, or 0: 16 queries per workgroup
+constexpr long long kQMaxWorkgroups = 1LL << 23;  // of one launch (a grid holds fewer than 2^32 threads)
+struct QAttnPlan {
+  int qh, splits;        // qh: 32-query halves per wave, or 0: 16 queries per workgroup
+  long long workgroups;  // a plan of more than kQMaxWorkgroups is not launched
+};
+// Query rows of the chains: offsets [chains + 1] on the host, or null: `tokens` rows each.
 QAttnPlan plan_qattention(const int *offsets, int chains, int heads, int tokens);
-hipError_t launch_qattention(const QAttnArgs &a, int chains, int max_rows, int qh, hipStream_t s);
+hipError_t launch_qattention(const QAttnArgs &a, int chains, const QAttnPlan &p, hipStream_t s);
 hipError_t launch_qattention_combine(const QAttnArgs &a, hipStream_t s);  // (splits > 1)
 
 // ------------------------------------------------------------------ device side

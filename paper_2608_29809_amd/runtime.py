@@ -198,6 +198,7 @@ class RegionCacheModel:
         from .quant import quantize
         if not enable:
             abi.rc_set_quant_weights(self.ctx, None)
+            torch.cuda.synchronize(self.device)  # (steps of any stream may still read them)
             self._quant = None
             return
         keep, layers = [], (abi.rc_quant_layer * self.L)()
@@ -206,6 +207,7 @@ class RegionCacheModel:
                 keep.append(quantize(t, 128))
                 setattr(layers[i], f, keep[-1].struct())
         abi.rc_set_quant_weights(self.ctx, layers)
+        torch.cuda.synchronize(self.device)  # (steps of other streams read them; earlier ones those that they replace)
         self._quant = keep
 
     def staging(self, batch: int) -> torch.Tensor:

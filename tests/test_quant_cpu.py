@@ -153,7 +153,7 @@ def test_attention_refusals():
 
 # ------------------------------------------------------------------ steps on an 8-bit pool
 
-def make_ctx(dtype=abi.RC_BF16, layers=2):
+def make_ctx(dtype=abi.RC_BF16, layers=2, grid=(32, 32)):
     L = (abi.rc_layer_weights * layers)()
     for i in range(layers):
         for f in abi.LAYER_FIELDS:
@@ -162,7 +162,7 @@ def make_ctx(dtype=abi.RC_BF16, layers=2):
     w.layers = C.cast(L, C.POINTER(abi.rc_layer_weights))
     for f in abi.GLOBAL_FIELDS:
         setattr(w, f, FAKE)
-    cfg = abi.rc_model_config(1152, 16, 72, 4608, layers, 120, 4096, 32, 32, 4, 2, 8, dtype, 0, 1e-6)
+    cfg = abi.rc_model_config(1152, 16, 72, 4608, layers, 120, 4096, *grid, 4, 2, 8, dtype, 0, 1e-6)
     ctx = C.c_void_p()
     assert abi.LIB.rc_create(C.byref(cfg), C.byref(w), C.byref(ctx)) == 0
     return ctx, L
@@ -294,3 +294,28 @@ def test_plain_attention_against_softmax():
     k, w = f[0, 0, :, 0].reshape(-1, 72)[:100], f[0, 0, :, 1].reshape(-1, 72)[:100]
     ref = torch.softmax(torch.from_numpy(q) @ k.T * 0.1, -1) @ w
     np.testing.assert_allclose(o, ref.numpy(), rtol=1e-12)
+
+
+def test_attention_grid_limits():
+    """One long chain among very many: the grid holds the longest one's tiles for each."""
+    n = 32767
+    rows = aset([0, 1 << 20] + [(1 << 20) + i for i in range(1, n)], idx=None)
+    c = qcache(batch=n, heads=16, tokens=64, chain_stride=16 * 64 * 144, scale_stride=32)
+    f = abi.LIB.rc_qcache_attention
+    assert f(C.byref(c), C.byref(rows), None, FAKE, 1152, 0.1, FAKE, 1152, FAKE, 1 << 40, None) == -2
+    assert "too many" in abi.rc_last_error()
+    ctx, keep = make_ctx(grid=(128, 128))
+    nb, ws = abi.rc_quant_cache_bytes(ctx, n, 1), abi.rc_quant_workspace_bytes(ctx, 1 << 17, n)
+    rows = aset([0, 16384] + [16384 + i for i in range(1, n)])
+    assert abi.LIB.rc_reuse_step_quant(ctx, C.byref(abi.rc_cache_view(FAKE, nb, n, 1)), 0, C.byref(rows), C.byref(step_io()),
+                                       abi.RC_FUSE_UPDATE, FAKE, ws, None) == -2
+    assert "too many" in abi.rc_last_error()
+    abi.rc_destroy(ctx)
+
+
+@pytest.mark.parametrize("scale", [3.0e38, -2.4e38])
+def test_attention_scale_limit(scale):
+    """The scale times log2(e) has to be finite too."""
+    rows = aset([0, 5, 9], idx=None)
+    assert abi.LIB.rc_qcache_attention(C.byref(qcache()), C.byref(rows), None, FAKE, 288, scale, FAKE, 288, FAKE, 1 << 40,
+                                       None) == -1

@@ -562,7 +562,7 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
     g.a = a; g.as = as; g.lda = w.cols; g.as_ld = qw.scale_ld;
     g.w = (const uint8_t *)w.data; g.ws = w.scales; g.ldw = w.ld; g.ws_ld = w.scale_ld;
     g.M = R; g.N = w.rows; g.K = w.cols; g.bias = bias; g.ldo = w.rows;
-    return timed(c, cls, s, [&] { return rc::launch_qgemm(g, rc::plan_qgemm(g.M, g.N, g.K, epi), epi, false, s); });
+    return timed(c, cls, s, [&] { return rc::launch_qgemm(g, rc::plan_qgemm(g.M, g.N, g.K, epi, true), epi, false, s); });
   };
   rc::ChainRows q_rows{};
   rc::QAttnPlan q_plan{};
@@ -1527,7 +1527,8 @@ rc_status rc_qgemm(const rc_qmat *a, const rc_qmat *w, const float *bias, int32_
   g.w = (const uint8_t *)w->data; g.ws = w->scales; g.ldw = w->ld; g.ws_ld = w->scale_ld;
   g.M = a->rows; g.N = w->rows; g.K = a->cols; g.bias = bias; g.out = out; g.ldo = ldo;
   const rc::QGemmEpi epi = gelu ? rc::QG_GELU : rc::QG_STORE;
-  RC_HIP(rc::launch_qgemm(g, rc::plan_qgemm(g.M, g.N, g.K, epi), epi, out_dtype == RC_F32, (hipStream_t)stream));
+  const bool large = out_dtype == RC_BF16 && g.N % 8 == 0 && ldo % 8 == 0;
+  RC_HIP(rc::launch_qgemm(g, rc::plan_qgemm(g.M, g.N, g.K, epi, large), epi, out_dtype == RC_F32, (hipStream_t)stream));
   return RC_OK;
 }
 

@@ -21,6 +21,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace rc {
 
@@ -478,6 +479,331 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, 2) void qgemm_kernel(QGemmArgs
   }
 }
 
+// ------------------------------------------------------------------ whole chip
+
+// Lane groups 1 and 3 (of 16) of x change places with groups 0 and 2 of y.
+__device__ __forceinline__ void q_swap16(uint32_t &x, uint32_t &y) {
+  const auto r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+  x = r[0];
+  y = r[1];
+}
+// Lane groups 2 and 3 of x change places with groups 0 and 1 of y.
+__device__ __forceinline__ void q_swap32(uint32_t &x, uint32_t &y) {
+  const auto r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+  x = r[0];
+  y = r[1];
+}
+
+// gelu_tanh with one multiplication less.
+__device__ __forceinline__ float q_gelu(float x) {
+  constexpr float k = -2.0f * 0.7978845608028654f * 1.4426950408889634f;
+  return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * __builtin_fmaf(x * x, 0.044715f * k, k)));
+}
+// A copy of 4 bytes per lane to LDS.
+__device__ __forceinline__ void lds_dma4s(const void *from, unsigned lane_off, unsigned to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, %2" ::"v"(lane_off), "s"(to), "s"(from) : "memory", "m0");
+}
+// A copy of 16 bytes per lane to LDS base + PLACE (uniform), in as few instructions as fit between two products.
+template <int PLACE> __device__ __forceinline__ void lds_copy16(const void *from, unsigned lane_off, unsigned base) {
+  asm volatile("s_add_u32 m0, %1, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %3" ::"v"(lane_off), "s"(base), "n"(PLACE),
+               "s"(from) : "memory", "m0", "scc");
+}
+// 256 x 256 tiles, one workgroup of four waves per CU, 128 x 128 results per
+// wave (all 256 accumulation registers): a step of K, 64 matrix instructions or
+// 2048 clocks, takes 32 KB of fragments a wave and 64 KB of copies from memory,
+// where 128 x 128 tiles of 64 x 64 per wave take all that LDS gives and twice
+// the copies.  With one wave per SIMD nothing but the order of instructions
+// covers latency:
+// * stages of 128 of K in a ring of two.  A step's first half multiplies column
+//   by column and reads the rest of its W fragments at once; then the stage is
+//   in registers and its place takes the stage after next.  The second half
+//   multiplies row by row and reads the next stage's fragments into the
+//   registers of the rows that are done with.
+// * Copies are issued one between two products, every third product (all at
+//   once they hold a wave up for 1100 clocks a step; with a branch each, 400).
+// * The steps of a workgroup's tiles are one sequence: the last two steps of a
+//   tile copy the next one's first stages, which arrive during the epilogue.
+//   That needs no LDS: lanes exchange registers until they hold whole stores.
+// Bound by the matrix instructions in the loop (2330 clocks a step where few CUs
+// work; with all of them the power limit leaves 1.8 GHz), then by the epilogue's
+// vector instructions: LARGE_
+template <int EPI>
+__global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int tiles) {
+  constexpr int B = 256, F = 8, HALF = B * kQBlock, STAGE = 2 * HALF, NC = HALF / 4096;
+  constexpr bool GELU = EPI == QG_GELU || EPI == QG_GELU8;
+  // per slot: rows, W; behind the ring, per slot: the rows' scales, W's four; for two tiles: the bias
+  constexpr int SCALES = 2 * STAGE, BIAS = SCALES + 2 * 2 * B;
+  __shared__ __attribute__((aligned(1024))) char lds[BIAS + 2 * 4 * B];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __builtin_assume(wave >= 0 && wave < 4);
+  const int wm = wave >> 1, wn = wave & 1, l16 = lane & 15, lq = lane >> 4;
+  const int tiles_m = (g.M + B - 1) / B, tiles_n = (g.N + B - 1) / B, n = g.K / kQBlock;
+  // bands of GM row tiles, as above
+  constexpr int GM = 2048 / B;
+  auto place = [&](int p, int &m0, int &n0) {
+    const int L = xcd_logical_id(p, tiles);
+    const int band0 = L / (GM * tiles_n), gm = min(GM, tiles_m - band0 * GM), idx = L - band0 * GM * tiles_n;
+    m0 = __builtin_amdgcn_readfirstlane((band0 * GM + idx % gm) * B);
+    n0 = __builtin_amdgcn_readfirstlane(idx / gm * B);
+  };
+
+  const unsigned ring0 = __builtin_amdgcn_readfirstlane(lds_address(lds)), mine = ring0 + wave * 1024;
+
+  // The next stage to be copied: rows, W, their scales.
+  const int row8 = wave * 8 + (lane >> 3), chunk = ((lane & 7) ^ ((row8 >> 1) & 7)) * 16;
+  const uint8_t *c_a, *c_w, *c_as, *c_ws;
+  unsigned off_a[NC], off_w[NC];
+  int c_rows, by = kQBlock, as_by = g.as_ld, ws_by = g.ws_ld;
+  auto enter = [&](int m0, int n0) {  // a tile's first
+    c_a = g.a + m0 * g.lda;
+    c_w = g.w + n0 * g.ldw;
+    c_as = g.as + m0;
+    c_ws = g.ws + (n0 / kQBlock & ~3);
+    c_rows = g.M - 1 - m0;
+#pragma unroll
+    for (int q = 0; q < NC; ++q) {  // (rows behind the last are copies of it)
+      off_a[q] = __umul24((unsigned)min(row8 + q * 32, c_rows), (unsigned)g.lda) + chunk;
+      off_w[q] = __umul24((unsigned)min(row8 + q * 32, g.N - 1 - n0), (unsigned)g.ldw) + chunk;
+    }
+  };
+  auto copy_bias = [&](int n0, int which) {  // (a wave's 64 columns)
+    lds_dma4s(g.bias, (unsigned)min(n0 + wave * 64 + lane, g.N - 1) * 4u, ring0 + BIAS + which * 4 * B + wave * 256);
+  };
+  auto advance = [&]() {
+    c_a += by;
+    c_w += by;
+    c_as += as_by;
+    c_ws += ws_by;
+  };
+  // (the same by every wave, so that every wave has the same copies in flight)
+  auto copy_scales = [&](int slot) {
+    const unsigned to = ring0 + SCALES + slot * 2 * B;
+    lds_dma4s(c_as, (unsigned)min(lane * 4, c_rows & ~3), to);
+    lds_dma4s(c_ws, 0, to + B);
+  };
+  auto copy_a = [&](int slot, int q) {
+    switch (q) {
+#define RC_CASE(Q) case Q: return lds_copy16<Q * 4096>(c_a, off_a[Q], mine + slot * STAGE);
+      RC_CASE(0) RC_CASE(1) RC_CASE(2) RC_CASE(3) RC_CASE(4) RC_CASE(5) RC_CASE(6) RC_CASE(7)
+#undef RC_CASE
+    }
+  };
+  auto copy_w = [&](int slot, int q) {
+    switch (q) {
+#define RC_CASE(Q) case Q: return lds_copy16<HALF + Q * 4096>(c_w, off_w[Q], mine + slot * STAGE);
+      RC_CASE(0) RC_CASE(1) RC_CASE(2) RC_CASE(3) RC_CASE(4) RC_CASE(5) RC_CASE(6) RC_CASE(7)
+#undef RC_CASE
+    }
+  };
+
+  f32x4 acc[F][F];
+  const int sz = (l16 >> 1) & 7, c_lo = l16 * kQBlock + ((lq ^ sz) << 4), c_hi = l16 * kQBlock + (((lq + 4) ^ sz) << 4);
+  i32x8 a[F], w[F];
+  int ea[F], ew, ew_next;
+  auto frag = [&](const char *rows) {
+    return __builtin_shufflevector(*(const i32x4 *)(rows + c_lo), *(const i32x4 *)(rows + c_hi), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto read_a = [&](int slot, int i) {
+    a[i] = frag(lds + slot * STAGE + (wm * F + i) * 16 * kQBlock);
+    ea[i] = *(const uint8_t *)(lds + SCALES + slot * 2 * B + (wm * F + i) * 16 + l16);
+  };
+  auto read_w = [&](int slot, int j) { w[j] = frag(lds + slot * STAGE + HALF + (wn * F + j) * 16 * kQBlock); };
+  auto read_ew = [&](int slot, int byte) { return (int)*(const uint8_t *)(lds + SCALES + slot * 2 * B + B + byte); };
+
+  int m0, n0;
+  place(blockIdx.x, m0, n0);
+  enter(m0, n0);
+  if (g.bias) copy_bias(n0, 0);
+  else *(f32x2 *)(lds + BIAS + tid * 8) = f32x2{0.0f, 0.0f};
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    copy_scales(s);
+#pragma unroll
+    for (int q = 0; q < NC; ++q) copy_a(s, q);
+#pragma unroll
+    for (int q = 0; q < NC; ++q) copy_w(s, q);
+    advance();
+  }
+  wait_vm_q<2 + 2 * NC>();
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  ew = read_ew(0, (n0 / kQBlock & 3) + wn);
+#pragma unroll
+  for (int j = 0; j < F / 2; ++j) read_w(0, j);
+#pragma unroll
+  for (int i = 0; i < F; ++i) read_a(0, i);
+
+  int slot = 0, which = 0;
+  auto multiply = [&](int q, int j) {
+    acc[q][j] = q_mma<false>(w[j], a[q], acc[q][j], ew, ea[q]);
+    asm volatile("" : "+a"(acc[q][j]));  // (in its place)
+  };
+  constexpr int FROM = 13, EVERY = 3;  // products before the first copy, and between two
+  auto step = [&](int byte) {  // byte: W's scale of the next stage
+#pragma unroll
+    for (int t8 = 0; t8 < F; ++t8)
+#pragma unroll
+    for (int t1 = 0; t1 < F; ++t1) {
+      const int t = t8 * F + t1;
+      // the first half column by column, the second row by row
+      const int q = t < 32 ? t % F : (t - 32) / 4, j = t < 32 ? t / F : 4 + t % 4;
+      multiply(q, j);
+      if (t < 4) read_w(slot, 4 + t);
+      if (t == 11) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // every wave has all of this stage
+      if (t == 12) copy_scales(slot);
+      if (t >= FROM && t < FROM + EVERY * 2 * NC && (t - FROM) % EVERY == 0) {
+        const int c = (t - FROM) / EVERY;
+        if (c < NC) copy_a(slot, c);
+        else copy_w(slot, c - NC);
+      }
+      if (t == 31) {  // the next stage is there
+        wait_vm_q<2 + (32 - FROM + EVERY - 1) / EVERY>();
+        asm volatile("s_barrier" ::: "memory");
+      }
+      if (t >= 32 && t % 8 == 1) read_w(slot ^ 1, (t - 32) / 8);
+      if (t == 53) ew_next = read_ew(slot ^ 1, byte);
+      if (t >= 32 && j == 7) read_a(slot ^ 1, q);  // (behind the last stage: stale, never used)
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    ew = ew_next;
+    advance();
+    slot ^= 1;
+  };
+
+#pragma nounroll
+  for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+    int next_m0 = m0, next_n0 = n0;
+    if (t + (int)gridDim.x < tiles) place(t + gridDim.x, next_m0, next_n0);
+    const int byte = (n0 / kQBlock & 3) + wn, next_byte = (next_n0 / kQBlock & 3) + wn;
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+      for (int j = 0; j < F; ++j) {
+        acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        asm volatile("" : "+a"(acc[i][j]));
+      }
+    // (all but the last two steps copy from this tile, those from the next)
+    int i = 0;
+#pragma nounroll
+    for (int last = n - 2; i < n; last = n) {
+#pragma nounroll
+      for (; i < last; ++i) step(i + 1 < n ? byte : next_byte);
+      if (i < n) {
+        if (t + (int)gridDim.x < tiles) {
+          enter(next_m0, next_n0);
+          if (g.bias) copy_bias(next_n0, which ^ 1);
+        } else {  // no next one: the last stage again
+          c_a -= by;
+          c_w -= by;
+          c_as -= as_by;
+          c_ws -= ws_by;
+          by = as_by = ws_by = 0;
+        }
+      }
+    }
+
+    // lane (l16, lq) holds, of row i * 16 + l16, columns j * 16 + lq * 4 .. + 3
+    int my = lane;
+    asm volatile("" : "+v"(my));  // (nothing that follows is made ahead and kept)
+    const int lq = my >> 4, col0 = n0 + wn * 128, row0 = m0 + wm * 128 + (my & 15);
+    f32x4 bias[F];
+#pragma unroll
+    for (int j = 0; j < F; ++j) bias[j] = *(const f32x4 *)(lds + BIAS + which * 4 * B + (wn * 128 + j * 16 + lq * 4) * 4);
+    m0 = next_m0;
+    n0 = next_n0;
+    which ^= 1;
+    if constexpr (EPI == QG_RESID) {
+      f32x4 gate[F], x[2][F];
+      int packed[2];
+      auto load = [&](int i) {  // (a row block ahead; rows and columns behind the last: any valid ones)
+        const int row = min(row0 + i * 16, g.M - 1);
+        packed[i & 1] = g.packed[row];
+#pragma unroll
+        for (int j = 0; j < F; ++j) x[i & 1][j] = *(const f32x4 *)(g.X + (size_t)row * g.N + min(col0 + j * 16 + lq * 4, g.N - 4));
+      };
+#pragma unroll
+      for (int j = 0; j < F; ++j) {
+        const int col = min(col0 + j * 16 + lq * 4, g.N - 4);
+        gate[j] = *(const f32x4 *)(g.gate + col) + *(const f32x4 *)(g.gate2 + col);
+      }
+      load(0);
+#pragma unroll
+      for (int i = 0; i < F; ++i) {
+        if (i + 1 < F) load(i + 1);
+        const int row = row0 + i * 16;
+        if (row < g.M) {
+          bf16 *h = g.hslot + row_chain(packed[i & 1]) * g.chain_stride + (size_t)row_token(packed[i & 1]) * g.N;
+#pragma unroll
+          for (int j = 0; j < F; ++j) {
+            const int col = col0 + j * 16 + lq * 4;
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = x[i & 1][j][e] + gate[j][e] * (acc[i][j][e] + bias[j][e]);
+            if (col < g.N) {
+              *(f32x4 *)(g.X + (size_t)row * g.N + col) = v;
+              *(bf16x4 *)(h + col) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+            }
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < F; ++i) {
+        const int row = row0 + i * 16;
+        float v[F][4];
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[j][e] = acc[i][j][e] + bias[j][e];
+            if (GELU) v[j][e] = q_gelu(v[j][e]);
+          }
+        }
+        if constexpr (EPI == QG_GELU8) {
+          float m = 0.0f;
+#pragma unroll
+          for (int j = 0; j < F; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = fmaxf(m, q_magnitude(v[j][e]));
+          uint32_t m0_ = __float_as_uint(m), m1_ = m0_;
+          q_swap16(m0_, m1_);
+          m = half_swap_max(fmaxf(__uint_as_float(m0_), __uint_as_float(m1_)));
+          const int ex = q_exponent(m);
+          const float inv = q_inverse(ex);
+#pragma unroll
+          for (int h = 0; h < F; h += 4) {  // four blocks of 16 columns: lane group lq gets block h + lq
+            uint32_t d[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) d[k] = q_pack4(v[h + k], inv);
+            q_swap16(d[0], d[1]);
+            q_swap16(d[2], d[3]);
+            q_swap32(d[0], d[2]);
+            q_swap32(d[1], d[3]);
+            if (row < g.M && col0 < g.N)
+              *(u32x4 *)((uint8_t *)g.out + row * g.ldo + col0 + (h + lq) * 16) = u32x4{d[0], d[1], d[2], d[3]};
+          }
+          if (lq == 0 && row < g.M && col0 < g.N) g.out_scales[(size_t)(col0 / kQBlock) * g.out_scale_ld + row] = (uint8_t)ex;
+        } else {
+#pragma unroll
+          for (int j = 0; j < F; j += 2) {  // two blocks of 16 columns: eight in a row for each lane
+            uint32_t u[2][2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              u[k][0] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)v[j + k][0], (bf16)v[j + k][1]});
+              u[k][1] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)v[j + k][2], (bf16)v[j + k][3]});
+            }
+            q_swap16(u[0][0], u[1][0]);
+            q_swap16(u[0][1], u[1][1]);
+            const int col = col0 + (j + (lq & 1)) * 16 + (lq >> 1) * 8;
+            if (row < g.M && col < g.N)
+              __builtin_nontemporal_store(u32x4{u[0][0], u[0][1], u[1][0], u[1][1]}, (u32x4 *)((bf16 *)g.out + row * g.ldo + col));
+          }
+        }
+      }
+    }
+  }
+  wait_vm_q<0>();  // (the copies behind the last stage)
+}
+
 template <int EPI, typename OUT> static hipError_t launch_qg(const QGemmArgs &a, const QGemmPlan &p, hipStream_t s) {
   const long long n = ((long long)a.M + p.bm - 1) / p.bm * (((long long)a.N + p.bn - 1) / p.bn);
   if (n > 1 << 22) return hipErrorInvalidValue;  // (a grid holds fewer than 2^32 threads)
@@ -497,29 +823,41 @@ template <int EPI, typename OUT> static hipError_t launch_qg(const QGemmArgs &a,
   }
   if (tile == 64128) RC_QG(4, 2, 1, 4, 1, 3);
   if (tile == 128128) RC_QG(4, 4, 2, 2, 1, 2);
+  if constexpr (sizeof(OUT) == 2)
+    if (tile == 256256) {
+      if (a.K % kQBlock || a.K < 2 * kQBlock || a.N % 8 || a.ldo % 8) return hipErrorInvalidValue;
+      return rc_launch(qgemm_large_kernel<EPI>, dim3(std::min(tiles, 256u)), dim3(256), 0, s, a, (int)tiles);
+    }
 #undef RC_QG
 #undef RC_QG_SPLIT
   return hipErrorInvalidValue;
 }
 
 // The tile with the least estimated time: 5 us of ends, and for each step of K
-// the time of the workgroups that share a CU.  Measured, us: 1 x 4608 x 1152 6.5
-// (16 x 16), 64 x 4608 x 1152 7.4 (64 x 32; 32 x 32 8.9), 219 x 1000 x 1072 in
-// float32 6.6 (32 x 32; 64 x 32 8.1), 154 x 1152 x 4608 11.6 (64 x 32; 32 x 32
-// 13.0), 723 x 1152 x 4608 16.0 (64 x 64; 64 x 32 21), 723 x 4608 x 1152 14.0 (64 x
-// 128; 128 x 128 14.9, 64 x 64 26), 2458 x 4608 x 1152 30 (128 x 128; 64 x 128 35).
-QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi) {
-  struct Tile { int bm, bn, kg; double fixed, per; };  // us a step, and a step per workgroup of a CU
-  static constexpr Tile tiles[] = {{16, 16, 8, 0.0, 0.6}, {32, 32, 8, 0.0, 1.2}, {64, 32, 4, 0.0, 0.8},
-                                   {64, 64, 4, 0.0, 1.25}, {64, 128, 1, 0.15, 0.5}, {128, 128, 1, 0.3, 0.8}};
+// the time of the workgroups that share a CU, with an end of their own where
+// they are not all there at once.  Measured, us: 1 x 4608 x 1152 6.5 (16 x 16),
+// 64 x 4608 x 1152 7.4 (64 x 32; 32 x 32 8.9), 219 x 1000 x 1072 in float32 6.6
+// (32 x 32; 64 x 32 8.1), 154 x 1152 x 4608 11.6 (64 x 32; 32 x 32 13.0), 723 x
+// 1152 x 4608 16.0 (64 x 64; 64 x 32 21), 723 x 4608 x 1152 13.3 (64 x 128; 128 x
+// 128 14.9, 64 x 64 26), 2458 x 4608 x 1152 PLAN_, 4096 x 4608 x 1152 with GELU
+// 38 (128 x 128; 256 x 256, 288 tiles for 256 CUs, 41), 4096 x 3456 x 1152 23 (256
+// x 256; 128 x 128 27), 4096 x 1152 x 4608 34 (128 x 128; 256 x 256, 80 tiles, 45),
+// 16384 x 4608 x 1152 99 (256 x 256; 128 x 128 118), 16384 x 1152 x 4608 100 and 120.
+QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi, bool large) {
+  struct Tile { int bm, bn, kg; double fixed, per, end; };  // us a step, a step per workgroup of a CU, a workgroup
+  static constexpr Tile tiles[] = {{16, 16, 8, 0.0, 0.6, 0.0}, {32, 32, 8, 0.0, 1.2, 0.0}, {64, 32, 4, 0.0, 0.8, 0.0},
+                                   {64, 64, 4, 0.0, 1.25, 0.0}, {64, 128, 1, 0.15, 0.5, 0.0}, {128, 128, 1, 0.25, 0.68, 1.1},
+                                   {256, 256, 0, 0.0, 1.2, 5.5}};
   const int blocks = (K + kQBlock - 1) / kQBlock;
   QGemmPlan best{128, 128};
   double best_us = 1e30;
   for (const Tile &t : tiles) {
-    if ((epi == QG_GELU8 && t.bn != kQBlock) || (epi == QG_RESID && t.bm < 64)) continue;  // (tiles that have the epilogue)
+    if ((epi == QG_GELU8 && t.bn % kQBlock) || (epi == QG_RESID && t.bm < 64)) continue;  // (tiles that have the epilogue)
+    if (t.kg == 0 && (!large || K % kQBlock || K < 2 * kQBlock)) continue;
     const double wgs = std::ceil((double)M / t.bm) * std::ceil((double)N / t.bn) / 256;
-    const double load = t.kg > 1 ? std::ceil(wgs) : std::max(wgs, 1.0), steps = (blocks + t.kg - 1) / t.kg;
-    const double us = 5.0 + steps * (t.fixed + t.per * load);
+    const double load = t.kg == 1 ? std::max(wgs, 1.0) : std::ceil(wgs);  // (kg 0: one tile after the other)
+    const double steps = t.kg > 1 ? (blocks + t.kg - 1) / t.kg : blocks;
+    const double us = 5.0 + steps * (t.fixed + t.per * load) + t.end * load;
     if (us < best_us) {
       best_us = us;
       best = QGemmPlan{t.bm, t.bn};

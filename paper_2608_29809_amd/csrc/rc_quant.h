@@ -70,7 +70,8 @@ struct QGemmArgs {
   long long chain_stride;   // elements
 };
 struct QGemmPlan { int bm, bn; };  // workgroup tile
-QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi);
+// large: bfloat16 or 8-bit results, N and their row stride multiples of 8 (what 256 x 256 tiles need)
+QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi, bool large);
 hipError_t launch_qgemm(const QGemmArgs &a, const QGemmPlan &p, QGemmEpi epi, bool f32_out, hipStream_t s);
 
 struct QCacheArgs {

@@ -179,6 +179,47 @@ def test_qgemm_nan_stays_in_its_row_and_column(Q, m, f32):
     np.testing.assert_array_equal(np.isnan(y), bad)
 
 
+LARGE = [(3001, 4360, 640, 4360), (4500, 6000, 384, 6016)]  # 256 x 256 tiles: one round of workgroups, two; the last in gaps
+
+
+@pytest.mark.parametrize("m,n,k,ldo", LARGE)
+def test_qgemm_large(Q, m, n, k, ldo):
+    a, ea, w, ew = product(m, n, k, seed=m)
+    bias = rnd(torch.float32, n, seed=9)
+    buf = torch.full((m + 2, ldo), 77.0, dtype=torch.bfloat16, device="cuda")
+    A, W = matrix(Q, a, ea, 1, 32), matrix(Q, w, ew, 128, 16)  # (NaN codes between and behind the rows)
+    for gelu in (False, True):
+        Q.qgemm(A, W, dev(bias), gelu=gelu, out=buf[:m, :n])
+        check_product(buf[:m, :n], a, ea, w, ew, bias, gelu, False)
+    Q.qgemm(A, W, out=buf[:m, :n])
+    check_product(buf[:m, :n], a, ea, w, ew, None, False, False)
+    assert (buf[:, n:] == 77.0).all() and (buf[m:] == 77.0).all()
+
+
+def test_qgemm_large_nan_stays_in_its_row_and_column(Q):
+    m, n, k, _ = LARGE[0]
+    a, ea, w, ew = product(m, n, k, seed=6)
+    a[2, 100], a[3000, 639], w[33, 7], w[4359, 0] = np.nan, np.nan, np.nan, np.nan
+    y = Q.qgemm(matrix(Q, a, ea, 1), matrix(Q, w, ew, 128))
+    bad = torch.zeros(y.shape, dtype=torch.bool, device="cuda")
+    bad[[2, 3000]], bad[:, [33, 4359]] = True, True
+    assert torch.equal(torch.isnan(y), bad)
+
+
+@pytest.mark.parametrize("tile,m,n,k", [(1, 5, 48, 300), (1, 130, 64, 1152), (128, 5, 200, 384)])
+def test_qgemm_scale_views(Q, tile, m, n, k):
+    """Scales that are the last columns of a wider tensor, whose memory ends with them."""
+    k -= k % 16
+    a, ea, w, ew = product(m, n, k, seed=11)
+    A, W = matrix(Q, a, ea, 1), matrix(Q, w, ew, 128)
+    X = A if tile == 1 else W
+    wide = torch.full((X.scales.shape[0], 16 + X.scales.shape[1]), 0xFF, dtype=torch.uint8, device="cuda")
+    wide[:, 16:] = X.scales
+    X = Q.QuantMatrix(X.data, wide[:, 16:], tile)
+    y = Q.qgemm(X, W) if tile == 1 else Q.qgemm(A, X)
+    check_product(y, a, ea, w, ew, None, False, False)
+
+
 def test_qgemm_scales_far_apart(Q):
     """Blocks of one sum whose scales differ by 2^60, the large ones cancelling."""
     a, ea, w, ew = product(40, 48, 384, seed=7)

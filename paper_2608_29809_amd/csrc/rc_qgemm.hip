@@ -176,12 +176,10 @@ __global__ __launch_bounds__(64 * KG) void qgemm_split_kernel(QGemmArgs g) {
 //   waited for, a block's fragments are read while the block before is
 //   multiplied, in the registers that its fragments leave, and the groups' sums
 //   are joined in LDS in a fixed order.
-// What bounds it: for 16384 x 4608 x 1152 (128 x 128 tiles: 115 us, 132 with GELU;
-// 1.5 PFLOP/s at the 1.75 GHz that the power limit leaves) LDS, which gives 128
-// bytes per clock and takes 187 for 64 x 64 wave tiles with their copies, then
-// the epilogues.  256 x 256 tiles (64 x 128 per wave, 125 bytes per clock) have
-// one workgroup per CU: 111 and 133 us, and 128 instead of 105 at 16384 x 1152 x
-// 4608.  723 x 1152 x 4608 (64 x 64 tiles, KG = 4): 16 us, 34 with 128 x 128.
+// What bounds it: with 128 x 128 tiles (4096 x 4608 x 1152 with GELU: 38 us, 1.1
+// PFLOP/s) LDS, which gives 128 bytes per clock and takes 187 for 64 x 64 wave
+// tiles with their copies, then the epilogues; with KG = 4 the copies' latency
+// (723 x 1152 x 4608, 64 x 64 tiles: 16 us, 34 with 128 x 128).
 template <int FM, int FN, int WGM, int WGN, int KG, int S, int EPI, typename OUT>
 __global__ __launch_bounds__(64 * WGM * WGN * KG, 2) void qgemm_kernel(QGemmArgs g) {
   constexpr int NG = WGM * WGN, NW = NG * KG, BM = 16 * FM * WGM, BN = 16 * FN * WGN;
@@ -524,9 +522,11 @@ template <int PLACE> __device__ __forceinline__ void lds_copy16(const void *from
 // * The steps of a workgroup's tiles are one sequence: the last two steps of a
 //   tile copy the next one's first stages, which arrive during the epilogue.
 //   That needs no LDS: lanes exchange registers until they hold whole stores.
-// Bound by the matrix instructions in the loop (2330 clocks a step where few CUs
-// work; with all of them the power limit leaves 1.8 GHz), then by the epilogue's
-// vector instructions: LARGE_
+// 2330 clocks a step where few CUs work; with all of them the power limit leaves
+// 1.8 GHz.  A tile's epilogue takes 6500 clocks, 17500 with GELU, of nine steps'
+// 21000 at K = 1152, and nothing covers it (accumulators of a second tile find
+// no registers).  16384 x 4608 x 1152: 99 us (128 x 128 tiles 118), 104 with GELU
+// (134); 8192 x 8192 x 9216: 462 us, 2.7 PFLOP/s.
 template <int EPI>
 __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int tiles) {
   constexpr int B = 256, F = 8, HALF = B * kQBlock, STAGE = 2 * HALF, NC = HALF / 4096;
@@ -833,21 +833,21 @@ template <int EPI, typename OUT> static hipError_t launch_qg(const QGemmArgs &a,
   return hipErrorInvalidValue;
 }
 
-// The tile with the least estimated time: 5 us of ends, and for each step of K
-// the time of the workgroups that share a CU, with an end of their own where
-// they are not all there at once.  Measured, us: 1 x 4608 x 1152 6.5 (16 x 16),
-// 64 x 4608 x 1152 7.4 (64 x 32; 32 x 32 8.9), 219 x 1000 x 1072 in float32 6.6
-// (32 x 32; 64 x 32 8.1), 154 x 1152 x 4608 11.6 (64 x 32; 32 x 32 13.0), 723 x
-// 1152 x 4608 16.0 (64 x 64; 64 x 32 21), 723 x 4608 x 1152 13.3 (64 x 128; 128 x
-// 128 14.9, 64 x 64 26), 2458 x 4608 x 1152 PLAN_, 4096 x 4608 x 1152 with GELU
-// 38 (128 x 128; 256 x 256, 288 tiles for 256 CUs, 41), 4096 x 3456 x 1152 23 (256
-// x 256; 128 x 128 27), 4096 x 1152 x 4608 34 (128 x 128; 256 x 256, 80 tiles, 45),
-// 16384 x 4608 x 1152 99 (256 x 256; 128 x 128 118), 16384 x 1152 x 4608 100 and 120.
+// The tile with the least estimated time: 5 us of ends, and for every tile that
+// a CU has to do a time for each step of K and an end.  Tiles that two
+// workgroups of a CU work on (kg 1) count as pairs where there are few.
+// Measured, us: 1 x 4608 x 1152 6.5 (16 x 16), 154 x 1152 x 4608 10.7 (64 x 32; 32 x 32
+// 11.4, 16 x 16 15.4), 154 x 4608 x 1152 7.8 (64 x 64; 64 x 32 10.3, 64 x 128 9.4), 300 x
+// 4608 x 1152 9.7 (64 x 128; 64 x 64 13.0), 723 x 1152 x 4608 16 (64 x 64; 64 x 32 21);
+// and 64 x 128, 128 x 128 and 256 x 256 tiles: 723 x 4608 x 1152 13.3, 14.9 and -, 1639 x
+// 4608 x 1152 22.5, 16.4 and 21.2, 2401 x 4608 x 1152 32, 25.9 and 22.1, 3500 x 1152 x
+// 4608 31.1, 31.4 and 44.2, 4096 x 4608 x 1152 -, 38 and 41 (288 tiles for 256 CUs),
+// 5800 x 1152 x 4608 56, 38 and 46, 8192 x 1152 x 4608 77, 65 and 49, 16384 x 4608 x
+// 1152 -, 118 and 99.
 QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi, bool large) {
-  struct Tile { int bm, bn, kg; double fixed, per, end; };  // us a step, a step per workgroup of a CU, a workgroup
-  static constexpr Tile tiles[] = {{16, 16, 8, 0.0, 0.6, 0.0}, {32, 32, 8, 0.0, 1.2, 0.0}, {64, 32, 4, 0.0, 0.8, 0.0},
-                                   {64, 64, 4, 0.0, 1.25, 0.0}, {64, 128, 1, 0.15, 0.5, 0.0}, {128, 128, 1, 0.25, 0.68, 1.1},
-                                   {256, 256, 0, 0.0, 1.2, 5.5}};
+  struct Tile { int bm, bn, kg; double per, end; };  // us a step, a tile
+  static constexpr Tile tiles[] = {{16, 16, 8, 0.6, 0.0}, {32, 32, 8, 1.3, 0.0}, {64, 32, 4, 0.7, 0.0}, {64, 64, 4, 1.25, 0.0},
+                                   {64, 128, 1, 0.33, 0.6}, {128, 128, 1, 0.44, 1.0}, {256, 256, 0, 1.1, 6.5}};
   const int blocks = (K + kQBlock - 1) / kQBlock;
   QGemmPlan best{128, 128};
   double best_us = 1e30;
@@ -855,9 +855,9 @@ QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi, bool large) {
     if ((epi == QG_GELU8 && t.bn % kQBlock) || (epi == QG_RESID && t.bm < 64)) continue;  // (tiles that have the epilogue)
     if (t.kg == 0 && (!large || K % kQBlock || K < 2 * kQBlock)) continue;
     const double wgs = std::ceil((double)M / t.bm) * std::ceil((double)N / t.bn) / 256;
-    const double load = t.kg == 1 ? std::max(wgs, 1.0) : std::ceil(wgs);  // (kg 0: one tile after the other)
+    const double load = t.kg != 1 ? std::ceil(wgs) : wgs <= 1.0 ? 1.7 : wgs <= 2.0 ? 2.0 : std::max(1.35 * wgs, 3.2);
     const double steps = t.kg > 1 ? (blocks + t.kg - 1) / t.kg : blocks;
-    const double us = 5.0 + steps * (t.fixed + t.per * load) + t.end * load;
+    const double us = 5.0 + load * (steps * t.per + t.end);
     if (us < best_us) {
       best_us = us;
       best = QGemmPlan{t.bm, t.bn};

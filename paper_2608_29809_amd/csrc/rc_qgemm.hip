@@ -705,20 +705,22 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
     int my = lane;
     asm volatile("" : "+v"(my));  // (nothing that follows is made ahead and kept)
     const int lq = my >> 4, col0 = n0 + wn * 128, row0 = m0 + wm * 128 + (my & 15);
-    f32x4 bias[F];
-#pragma unroll
-    for (int j = 0; j < F; ++j) bias[j] = *(const f32x4 *)(lds + BIAS + which * 4 * B + (wn * 128 + j * 16 + lq * 4) * 4);
+    const char *bias_at = lds + BIAS + which * 4 * B + (wn * 128 + lq * 4) * 4;
     m0 = next_m0;
     n0 = next_n0;
     which ^= 1;
     if constexpr (EPI == QG_RESID) {
-      f32x4 gate[F], x[2][F];
+      // half a row block of 16 at a time, its X and place loaded one half ahead
+      // (rows and columns behind the last: any valid ones)
+      constexpr int H = F / 2;
+      f32x4 gate[F], x[2][H];
       int packed[2];
-      auto load = [&](int i) {  // (a row block ahead; rows and columns behind the last: any valid ones)
-        const int row = min(row0 + i * 16, g.M - 1);
-        packed[i & 1] = g.packed[row];
+      auto load = [&](int u) {
+        const int row = min(row0 + u / 2 * 16, g.M - 1);
+        packed[u & 1] = g.packed[row];
 #pragma unroll
-        for (int j = 0; j < F; ++j) x[i & 1][j] = *(const f32x4 *)(g.X + (size_t)row * g.N + min(col0 + j * 16 + lq * 4, g.N - 4));
+        for (int j = 0; j < H; ++j)
+          x[u & 1][j] = *(const f32x4 *)(g.X + (size_t)row * g.N + min(col0 + (u % 2 * H + j) * 16 + lq * 4, g.N - 4));
       };
 #pragma unroll
       for (int j = 0; j < F; ++j) {
@@ -727,25 +729,37 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
       }
       load(0);
 #pragma unroll
-      for (int i = 0; i < F; ++i) {
-        if (i + 1 < F) load(i + 1);
-        const int row = row0 + i * 16;
-        if (row < g.M) {
-          bf16 *h = g.hslot + row_chain(packed[i & 1]) * g.chain_stride + (size_t)row_token(packed[i & 1]) * g.N;
+      for (int i = 0; i < F; ++i)
 #pragma unroll
-          for (int j = 0; j < F; ++j) {
-            const int col = col0 + j * 16 + lq * 4;
-            f32x4 v;
+        for (int half = 0; half < 2; ++half) {
+          const int u = i * 2 + half, row = row0 + i * 16;
+          __builtin_amdgcn_sched_barrier(0);
+          if (u + 1 < 2 * F) load(u + 1);
+          bf16 *h = g.hslot + row_chain(packed[u & 1]) * g.chain_stride + (size_t)row_token(packed[u & 1]) * g.N;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = x[i & 1][j][e] + gate[j][e] * (acc[i][j][e] + bias[j][e]);
-            if (col < g.N) {
-              *(f32x4 *)(g.X + (size_t)row * g.N + col) = v;
-              *(bf16x4 *)(h + col) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+          for (int j = half * H; j < half * H + H; j += 2) {
+            uint32_t y[2][2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int col = col0 + (j + k) * 16 + lq * 4;
+              const f32x4 bias = *(const f32x4 *)(bias_at + (j + k) * 64);
+              f32x4 v;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = x[u & 1][j + k - half * H][e] + gate[j + k][e] * (acc[i][j + k][e] + bias[e]);
+              if (row < g.M && col < g.N) *(f32x4 *)(g.X + (size_t)row * g.N + col) = v;
+              y[k][0] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)v[0], (bf16)v[1]});
+              y[k][1] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)v[2], (bf16)v[3]});
             }
+            q_swap16(y[0][0], y[1][0]);
+            q_swap16(y[0][1], y[1][1]);
+            const int col = col0 + (j + (lq & 1)) * 16 + (lq >> 1) * 8;
+            if (row < g.M && col < g.N) __builtin_nontemporal_store(u32x4{y[0][0], y[0][1], y[1][0], y[1][1]}, (u32x4 *)(h + col));
           }
         }
-      }
     } else {
+      f32x4 bias[F];
+#pragma unroll
+      for (int j = 0; j < F; ++j) bias[j] = *(const f32x4 *)(bias_at + j * 64);
 #pragma unroll
       for (int i = 0; i < F; ++i) {
         const int row = row0 + i * 16;
@@ -834,19 +848,19 @@ template <int EPI, typename OUT> static hipError_t launch_qg(const QGemmArgs &a,
 }
 
 // The tile with the least estimated time: 5 us of ends, and for every tile that
-// a CU has to do a time for each step of K and an end.  Tiles that two
-// workgroups of a CU work on (kg 1) count as pairs where there are few.
-// Measured, us: 1 x 4608 x 1152 6.5 (16 x 16), 154 x 1152 x 4608 10.7 (64 x 32; 32 x 32
-// 11.4, 16 x 16 15.4), 154 x 4608 x 1152 7.8 (64 x 64; 64 x 32 10.3, 64 x 128 9.4), 300 x
-// 4608 x 1152 9.7 (64 x 128; 64 x 64 13.0), 723 x 1152 x 4608 16 (64 x 64; 64 x 32 21);
-// and 64 x 128, 128 x 128 and 256 x 256 tiles: 723 x 4608 x 1152 13.3, 14.9 and -, 1639 x
-// 4608 x 1152 22.5, 16.4 and 21.2, 2401 x 4608 x 1152 32, 25.9 and 22.1, 3500 x 1152 x
-// 4608 31.1, 31.4 and 44.2, 4096 x 4608 x 1152 -, 38 and 41 (288 tiles for 256 CUs),
-// 5800 x 1152 x 4608 56, 38 and 46, 8192 x 1152 x 4608 77, 65 and 49, 16384 x 4608 x
-// 1152 -, 118 and 99.
+// a CU has to do a time for each step of K and an end.  Workgroups of small
+// tiles (kg 8) share a CU; those of kg 1 count as pairs where there are few.
+// Measured, us (kernels alone): 16 x 16, 32 x 32, 64 x 32 and 64 x 64 tiles 1 x 4608 x
+// 1152 4.6, 4.6, 6.0, 7.2; 16 x 1152 x 4608 7.4, 9.6, 10.4, 13.0; 64 x 4608 x 1152 8.7, 7.3,
+// 6.0, 7.4; 200 x 1152 x 640 5.9, 4.4, 5.4, 6.5; 200 x 1152 x 4608 19.7, 12.0, 11.4, 13.6;
+// 723 x 1152 x 4608 -, -, 21, 15.  With launches, 64 x 128, 128 x 128 and 256 x 256:
+// 723 x 4608 x 1152 13.3, 14.9, -; 1639 x 4608 x 1152 22.5, 16.4, 21.2; 2401 x 4608 x 1152
+// 32, 25.9, 22.1; 3500 x 1152 x 4608 31.1, 31.4, 44.2; 4096 x 4608 x 1152 -, 38, 41 (288
+// tiles for 256 CUs); 5800 x 1152 x 4608 56, 38, 46; 8192 x 1152 x 4608 77, 65, 49;
+// 16384 x 4608 x 1152 -, 118, 99.
 QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi, bool large) {
   struct Tile { int bm, bn, kg; double per, end; };  // us a step, a tile
-  static constexpr Tile tiles[] = {{16, 16, 8, 0.6, 0.0}, {32, 32, 8, 1.3, 0.0}, {64, 32, 4, 0.7, 0.0}, {64, 64, 4, 1.25, 0.0},
+  static constexpr Tile tiles[] = {{16, 16, 8, 1.0, 0.0}, {32, 32, 8, 1.7, 0.0}, {64, 32, 4, 0.65, 1.2}, {64, 64, 4, 0.85, 1.9},
                                    {64, 128, 1, 0.33, 0.6}, {128, 128, 1, 0.44, 1.0}, {256, 256, 0, 1.1, 6.5}};
   const int blocks = (K + kQBlock - 1) / kQBlock;
   QGemmPlan best{128, 128};
@@ -855,7 +869,9 @@ QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi, bool large) {
     if ((epi == QG_GELU8 && t.bn % kQBlock) || (epi == QG_RESID && t.bm < 64)) continue;  // (tiles that have the epilogue)
     if (t.kg == 0 && (!large || K % kQBlock || K < 2 * kQBlock)) continue;
     const double wgs = std::ceil((double)M / t.bm) * std::ceil((double)N / t.bn) / 256;
-    const double load = t.kg != 1 ? std::ceil(wgs) : wgs <= 1.0 ? 1.7 : wgs <= 2.0 ? 2.0 : std::max(1.35 * wgs, 3.2);
+    const double load = t.kg == 8   ? std::max(1.3 * wgs, 1.0)
+                        : t.kg != 1 ? std::ceil(wgs)
+                        : wgs <= 1.0 ? 1.7 : wgs <= 2.0 ? 2.0 : std::max(1.35 * wgs, 3.2);
     const double steps = t.kg > 1 ? (blocks + t.kg - 1) / t.kg : blocks;
     const double us = 5.0 + load * (steps * t.per + t.end);
     if (us < best_us) {

@@ -140,7 +140,7 @@ def check_product(y, a, ea, w, ew, bias, gelu, f32):
 
 SIZES = [(1, 4608, 1152), (1, 1, 16), (2, 7, 48), (5, 130, 128), (17, 16, 400), (128, 128, 256), (129, 144, 4608),
          (33, 1152, 1152), (219, 1000, 1072), (723, 300, 1152), (64, 4608, 144), (300, 257, 640),
-         (600, 1150, 1040), (777, 2300, 272), (2999, 2050, 400)]
+         (600, 1150, 1040), (777, 2300, 272), (2999, 2050, 400), (200, 1152, 640), (199, 1101, 1008)]
 
 
 @pytest.mark.parametrize("f32", [False, True])

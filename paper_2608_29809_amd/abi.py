@@ -155,17 +155,14 @@ def rc_last_error() -> str:
     return LIB.rc_last_error().decode()
 
 
-def _chk(name, st):
-    if st != RC_OK:
-        raise RcError(st, name, rc_last_error())
-    return st
-
-
 def _wrap(name):
     f = getattr(LIB, name)
 
     def call(*args):
-        return _chk(name, f(*args))
+        st = f(*args)
+        if st != RC_OK:
+            raise RcError(st, name, rc_last_error())
+        return st
 
     call.__name__ = name
     call.__doc__ = f"Forwards to the C function {name} (include/regioncache.h); raises RcError on failure."

@@ -31,10 +31,13 @@ HEAD_DIM = 72
 BLOCK = 128      # columns (and a weight's rows) that share a scale
 KEY_BLOCK = 64   # tokens of a cache block
 _DTYPES = {torch.float32: abi.RC_F32, torch.bfloat16: abi.RC_BF16}
+_F8, _U8 = torch.float8_e4m3fn, torch.uint8
 _SCALE = 1.0 / math.sqrt(HEAD_DIM)
 
-
-_raw_stream = torch._C._cuda_getCurrentRawStream  # (torch.cuda.current_stream takes 2.8 us of a call's 9)
+# The kernels of small calls take 3 to 7 us, a launch 3.2, so the host's time is a
+# call's time: torch.cuda.current_stream would add 2.8 us, current_device 0.2, sizes
+# as a tuple 0.35 to each torch.empty.
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:
@@ -44,24 +47,23 @@ def _dtype(t: torch.Tensor, what: str) -> int:
     return d
 
 
-def _on_gpu(first: torch.Tensor, *others: Optional[torch.Tensor]) -> torch.device:
-    """The one GPU that holds the tensors."""
-    dev = first.device
-    if dev.type != "cuda":
-        raise ValueError(f"the tensors must be on the GPU, not on {dev}")
+def _on_gpu(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
+    """Index of the one GPU that holds the tensors."""
+    if not first.is_cuda:
+        raise ValueError(f"the tensors must be on the GPU, not on {first.device}")
+    index = first.get_device()
     for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device}")
-    return dev
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
+    return index
 
 
-def _call(f, device: torch.device, *args):
-    """f(*args, stream) with `device` current and its current stream."""
-    index = device.index
-    if index == torch.cuda.current_device():
+def _call(f, index: int, *args):
+    """f(*args, stream) with GPU `index` current and its current stream."""
+    if index == _current_device():
         f(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             f(*args, _raw_stream(index))
 
 
@@ -82,38 +84,46 @@ class QuantMatrix:
     [column blocks, row blocks rounded up to 16], block_rows 1 or 128.  Views
     of rows are given as data[:n] with the same scales."""
 
-    __slots__ = ("data", "scales", "block_rows")
+    __slots__ = ("_data", "_scales", "_block_rows", "_struct")
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor, block_rows: int):
-        if data.dtype != torch.float8_e4m3fn or data.dim() != 2:
+        if data.dtype != _F8 or data.dim() != 2:
             raise ValueError("data must be float8_e4m3fn [rows, cols]")
-        if scales.dtype != torch.uint8 or scales.dim() != 2 or (scales.stride(1) != 1 and scales.shape[1] > 1):
+        if scales.dtype != _U8 or scales.dim() != 2 or not (scales.is_contiguous() or scales.stride(1) == 1):
             raise ValueError("scales must be uint8 [column blocks, row blocks] with contiguous rows")
         if block_rows != 1 and block_rows != BLOCK:
             raise ValueError(f"block_rows {block_rows} is not 1 or {BLOCK}")
         (rows, cols), (col_blocks, row_blocks) = data.shape, scales.shape
-        if col_blocks != -(-cols // BLOCK) or row_blocks < -(-rows // block_rows) or row_blocks % 16:
+        if rows >> 31 or col_blocks != -(-cols // BLOCK) or row_blocks < -(-rows // block_rows) or row_blocks % 16:
             raise ValueError(f"scales {tuple(scales.shape)} do not cover data {tuple(data.shape)} (row blocks padded to 16)")
         _on_gpu(data, scales)
-        self.data, self.scales, self.block_rows = data, scales, block_rows
+        ld = cols if data.is_contiguous() else _ld(data, rows, cols, "data")
+        self._data, self._scales, self._block_rows = data, scales, block_rows
+        self._struct = abi.rc_qmat(data.data_ptr(), scales.data_ptr(), ld, rows, cols,
+                                   row_blocks if col_blocks == 1 else scales.stride(0), block_rows)
+
+    # (read-only: the C structure is made once)
+    data = property(lambda self: self._data)
+    scales = property(lambda self: self._scales)
+    block_rows = property(lambda self: self._block_rows)
 
     @classmethod
     def alloc(cls, rows: int, cols: int, block_rows: int = 1, device="cuda") -> "QuantMatrix":
         if block_rows != 1 and block_rows != BLOCK:
             raise ValueError(f"block_rows {block_rows} is not 1 or {BLOCK}")
+        if rows >> 31 or cols >> 31:
+            raise ValueError(f"{rows} x {cols} is too large")
         m = cls.__new__(cls)
         row_blocks = -(-rows // block_rows)
-        m.data = torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=device)
-        m.scales = torch.empty((-(-cols // BLOCK), row_blocks + -row_blocks % 16), dtype=torch.uint8, device=device)
-        m.block_rows = block_rows
+        row_blocks += -row_blocks % 16
+        m._data = data = torch.empty(rows, cols, dtype=_F8, device=device)
+        m._scales = scales = torch.empty(-(-cols // BLOCK), row_blocks, dtype=_U8, device=device)
+        m._block_rows = block_rows
+        m._struct = abi.rc_qmat(data.data_ptr(), scales.data_ptr(), cols, rows, cols, row_blocks, block_rows)
         return m
 
     def struct(self) -> abi.rc_qmat:
-        rows, cols = self.data.shape
-        col_blocks, row_blocks = self.scales.shape
-        scale_ld = row_blocks if col_blocks == 1 else self.scales.stride(0)
-        return abi.rc_qmat(self.data.data_ptr(), self.scales.data_ptr(), _ld(self.data, rows, cols, "data"), rows, cols,
-                           scale_ld, self.block_rows)
+        return self._struct
 
 
 class QuantCache:
@@ -122,13 +132,13 @@ class QuantCache:
     `scales` uint8 [batch, heads, blocks, 2].  Chains may be any multiple of
     16 bytes apart; within a chain the cache is contiguous."""
 
-    __slots__ = ("data", "scales", "batch", "heads", "tokens")
+    __slots__ = ("_data", "_scales", "_struct", "batch", "heads", "tokens")
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor):
         shape = data.shape
-        if data.dtype != torch.float8_e4m3fn or len(shape) != 6 or shape[3:] != (2, KEY_BLOCK, HEAD_DIM):
+        if data.dtype != _F8 or len(shape) != 6 or shape[3:] != (2, KEY_BLOCK, HEAD_DIM):
             raise ValueError(f"data must be float8_e4m3fn [batch, heads, blocks, 2, {KEY_BLOCK}, {HEAD_DIM}]")
-        if scales.dtype != torch.uint8 or scales.shape != shape[:4]:
+        if scales.dtype != _U8 or scales.shape != shape[:4]:
             raise ValueError("scales must be uint8 [batch, heads, blocks, 2]")
         batch, heads, blocks = shape[:3]
         if not (batch and heads and blocks):
@@ -136,8 +146,14 @@ class QuantCache:
         if not (data.is_contiguous() or data[0].is_contiguous()) or not (scales.is_contiguous() or scales[0].is_contiguous()):
             raise ValueError("a chain of the cache must be contiguous")
         _on_gpu(data, scales)
-        self.data, self.scales = data, scales
+        self._data, self._scales = data, scales
         self.batch, self.heads, self.tokens = batch, heads, blocks * KEY_BLOCK
+        self._struct = abi.rc_qcache(data.data_ptr(), scales.data_ptr(), data.stride(0), scales.stride(0), batch, heads,
+                                     self.tokens)
+
+    # (read-only: the C structure is made once)
+    data = property(lambda self: self._data)
+    scales = property(lambda self: self._scales)
 
     @classmethod
     def alloc(cls, batch: int, heads: int, tokens: int, device="cuda") -> "QuantCache":
@@ -149,8 +165,7 @@ class QuantCache:
                    torch.zeros(shape, dtype=torch.uint8, device=device))
 
     def struct(self) -> abi.rc_qcache:
-        return abi.rc_qcache(self.data.data_ptr(), self.scales.data_ptr(), self.data.stride(0), self.scales.stride(0),
-                             self.batch, self.heads, self.tokens)
+        return self._struct
 
 
 def quantize(x: torch.Tensor, block_rows: int = 1, out: Optional[QuantMatrix] = None) -> QuantMatrix:
@@ -161,16 +176,16 @@ def quantize(x: torch.Tensor, block_rows: int = 1, out: Optional[QuantMatrix] = 
     if x.dim() != 2:
         raise ValueError(f"x is {tuple(x.shape)}, not [rows, cols]")
     rows, cols = x.shape
-    ldx = _ld(x, rows, cols, "x")
+    ldx = cols if x.is_contiguous() else _ld(x, rows, cols, "x")
     if out is None:
-        dev = _on_gpu(x)
-        out = QuantMatrix.alloc(rows, cols, block_rows, dev)
+        index = _on_gpu(x)
+        out = QuantMatrix.alloc(rows, cols, block_rows, x.device)
     else:
-        dev = _on_gpu(x, out.data)
+        index = _on_gpu(x, out.data)
         if out.data.shape != x.shape or out.block_rows != block_rows:
             raise ValueError("out has another shape or other blocks")
     if rows:
-        _call(abi.rc_quantize, dev, x.data_ptr(), dtype, ldx, C.byref(out.struct()))
+        _call(abi.rc_quantize, index, x.data_ptr(), dtype, ldx, C.byref(out._struct))
     return out
 
 
@@ -178,18 +193,20 @@ def qgemm(a: QuantMatrix, w: QuantMatrix, bias: Optional[torch.Tensor] = None, g
           dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """act(a w^T + bias): a [m, k] with block_rows 1, w [n, k] with block_rows
     128, bias float32 [n]; the result [m, n] in dtype (or in out)."""
-    m, n = a.data.shape[0], w.data.shape[0]
+    A, W = a._struct, w._struct
+    m, n = A.rows, W.rows
     if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,) or not bias.is_contiguous()):
         raise ValueError(f"bias must be contiguous float32 [{n}]")
     if out is None:
         if dtype not in _DTYPES:
             raise ValueError(f"dtype {dtype} is not float32 or bfloat16")
-        out = torch.empty((m, n), dtype=dtype, device=a.data.device)
-    ldo = _ld(out, m, n, "out")
-    dev = _on_gpu(a.data, w.data, bias, out)
+        out, ldo = torch.empty(m, n, dtype=dtype, device=a.data.device), n
+    else:
+        ldo = _ld(out, m, n, "out")
+    index = _on_gpu(a.data, w.data, bias, out)
     if m:
-        _call(abi.rc_qgemm, dev, C.byref(a.struct()), C.byref(w.struct()), None if bias is None else bias.data_ptr(),
-              1 if gelu else 0, out.data_ptr(), _dtype(out, "out"), ldo)
+        _call(abi.rc_qgemm, index, C.byref(A), C.byref(W), None if bias is None else bias.data_ptr(), 1 if gelu else 0,
+              out.data_ptr(), _dtype(out, "out"), ldo)
     return out
 
 
@@ -201,9 +218,9 @@ def qcache_store(cache: QuantCache, active: ActiveSet, k: torch.Tensor, v: torch
     ld = _ld(k, rows, cols, "k")
     if v.dtype != k.dtype or _ld(v, rows, cols, "v") != ld:
         raise ValueError("k and v must have one type and row stride")
-    dev = _on_gpu(cache.data, k, v, active.idx, active.offsets)
+    index = _on_gpu(cache.data, k, v, active.idx, active.offsets)
     if rows:
-        _call(abi.rc_qcache_store, dev, C.byref(cache.struct()), C.byref(active.struct()), k.data_ptr(), v.data_ptr(), dtype, ld)
+        _call(abi.rc_qcache_store, index, C.byref(cache._struct), C.byref(active.struct()), k.data_ptr(), v.data_ptr(), dtype, ld)
 
 
 def qcache_attention(cache: QuantCache, rows: ActiveSet, q: torch.Tensor, scale: Optional[float] = None,
@@ -215,20 +232,20 @@ def qcache_attention(cache: QuantCache, rows: ActiveSet, q: torch.Tensor, scale:
     cols, total = cache.heads * HEAD_DIM, rows.total
     if q.dtype != torch.bfloat16:
         raise ValueError(f"q is {q.dtype}, not bfloat16")
-    ldq = _ld(q, total, cols, "q")
+    ldq = cols if q.shape == (total, cols) and q.is_contiguous() else _ld(q, total, cols, "q")
     if key_len is not None and (key_len.dtype != torch.int32 or key_len.shape != (cache.batch,) or not key_len.is_contiguous()):
         raise ValueError(f"key_len must be contiguous int32 [{cache.batch}]")
     if out is None:
-        out = torch.empty((total, cols), dtype=torch.bfloat16, device=q.device)
+        out = torch.empty(total, cols, dtype=torch.bfloat16, device=q.device)
     elif out.dtype != torch.bfloat16:
         raise ValueError(f"out is {out.dtype}, not bfloat16")
     ldo = _ld(out, total, cols, "out")
-    dev = _on_gpu(cache.data, q, out, key_len, rows.offsets)
+    index = _on_gpu(cache.data, q, out, key_len, rows.offsets)
     if total:
-        c, s = cache.struct(), rows.struct()
+        c, s = cache._struct, rows.struct()
         nbytes = abi.rc_qcache_attention_scratch_bytes(C.byref(c), C.byref(s))
-        scratch = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-        _call(abi.rc_qcache_attention, dev, C.byref(c), C.byref(s), None if key_len is None else key_len.data_ptr(),
+        scratch = torch.empty(nbytes, dtype=_U8, device=q.device) if nbytes else None
+        _call(abi.rc_qcache_attention, index, C.byref(c), C.byref(s), None if key_len is None else key_len.data_ptr(),
               q.data_ptr(), ldq, _SCALE if scale is None else float(scale), out.data_ptr(), ldo,
               scratch.data_ptr() if nbytes else None, nbytes)
     return out

@@ -52,8 +52,7 @@ class ActiveSet:
         return cls(idx, torch.tensor(offs, dtype=torch.int32, device=device), offs)
 
     def struct(self):
-        return abi.rc_active_set(self.idx.data_ptr(), self.offsets.data_ptr(),
-                                 C.cast(self.host, C.POINTER(C.c_int32)), self.batch)
+        return abi.rc_active_set(self.idx.data_ptr(), self.offsets.data_ptr(), self.host, self.batch)
 
 
 class CacheBuffer:

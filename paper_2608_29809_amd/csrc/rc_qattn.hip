@@ -409,18 +409,23 @@ template <int QH> __global__ __launch_bounds__(256, 2) void qattn_kernel(QAttnAr
 }
 
 // Few queries (at most 16 of a chain per workgroup): bound by the cache's
-// bytes, so each wave streams tiles of its own (every fourth of the key range)
-// through a ring of two without a barrier, with a running maximum, and the four
-// waves' results are joined in LDS.  16x16x32 blocks: rows m of two 16-key
+// bytes, so each of eight waves streams tiles of its own (every eighth of the
+// key range) through a ring of two without a barrier, with a running maximum,
+// and the waves' results are joined in LDS.  (Two workgroups of four waves on a
+// CU need twice the key splits: 64 queries of 4096 keys 14.0 instead of 13.3 us,
+// 33 of 16384 22.5 instead of 21.1.)  One query of 16384 keys: 15.6 us with its
+// combine, 38 MB or 7.4 us of the cache; 13 splits, in which a wave takes two or
+// three tiles, then the ends and the second launch.  16x16x32 blocks: rows m of two 16-key
 // operands are keys (m>>2)*8 + (m&3) and those + 4 of 32, so that a lane's
 // eight scores are those of the eight keys that PV takes from it.
-__global__ __launch_bounds__(256, 2) void qattn_few_kernel(QAttnArgs a) {
-  constexpr int D = kHeadDim, RAW = 2 * kQTileBytes, STAGES = 2;
-  __shared__ __attribute__((aligned(1024))) char lds[4 * STAGES * RAW + 64];
-  __shared__ float wave_m[4][16], wave_l[4][16];
-  char *ones_chunk = lds + 4 * STAGES * RAW;  // read in place of value dims 72..79
+constexpr int kFewWaves = 8;
+__global__ __launch_bounds__(64 * kFewWaves, 2) void qattn_few_kernel(QAttnArgs a) {
+  constexpr int D = kHeadDim, RAW = 2 * kQTileBytes, STAGES = 2, W = kFewWaves;
+  __shared__ __attribute__((aligned(1024))) char lds[W * STAGES * RAW + 64];
+  __shared__ float wave_m[W][16], wave_l[W][16];
+  char *ones_chunk = lds + W * STAGES * RAW;  // read in place of value dims 72..79
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  __builtin_assume(wave >= 0 && wave < 4);
+  __builtin_assume(wave >= 0 && wave < W);
   const int l16 = lane & 15, lq = lane >> 4, heads = a.c.heads;
   int b, h, split, q0, r1;
   if (!locate(a, 16, b, h, split, q0, r1)) return;
@@ -428,19 +433,19 @@ __global__ __launch_bounds__(256, 2) void qattn_few_kernel(QAttnArgs a) {
   const int n_tiles = (keys + kQTokens - 1) / kQTokens;
   const int t_beg = (int)((long long)split * n_tiles / a.splits) + wave;
   const int t_end = (int)((long long)(split + 1) * n_tiles / a.splits);
-  const int n = t_beg < t_end ? (t_end - t_beg + 3) / 4 : 0;  // tiles t_beg + 4 i
+  const int n = t_beg < t_end ? (t_end - t_beg + W - 1) / W : 0;  // tiles t_beg + W i
   const uint8_t *data = a.c.data + b * a.c.chain_stride + ((size_t)h * (a.c.tokens / kQTokens) + t_beg) * RAW;
   const uint16_t *scales = (const uint16_t *)(a.c.scales + b * a.c.scale_chain_stride) + (size_t)h * (a.c.tokens / kQTokens) + t_beg;
   char *ring = lds + wave * STAGES * RAW;
   const unsigned ring0 = lds_address(ring);
   auto issue = [&](int slot, int i) {
-    const uint8_t *p = data + (size_t)i * 4 * RAW;
+    const uint8_t *p = data + (size_t)i * W * RAW;
 #pragma unroll
     for (int c = 0; c < RAW / 1024; ++c) lds_dma16s(p + c * 1024, lane * 16, ring0 + slot * RAW + c * 1024);
   };
   if (tid == 0) *(V16 *)ones_chunk = V16{{0x00000038u, 0u, 0u, 0u}};
   int sc = 0;  // scale bytes of 64 of the wave's tiles, one pair per lane
-  if (n > 0) sc = scales[4 * min(lane, n - 1)];
+  if (n > 0) sc = scales[W * min(lane, n - 1)];
   bf16x8 qf[3];
   const bf16 *qrow = a.q + min(q0 + l16, r1 - 1) * a.ldq + h * D;
 #pragma unroll
@@ -463,7 +468,7 @@ __global__ __launch_bounds__(256, 2) void qattn_few_kernel(QAttnArgs a) {
     if (i + 1 < n) wait_vm8<9>();
     else wait_vm8<0>();
     char *tile = ring + slot * RAW;
-    const int left = keys - (t_beg + 4 * i) * kQTokens;
+    const int left = keys - (t_beg + W * i) * kQTokens;
     if (left < kQTokens) {  // keys and values behind the last become zeros
       for (int c = left * (D / 8) + lane; c < kQTileBytes / 8; c += 64) {
         *(u32x2 *)(tile + c * 8) = u32x2{0u, 0u};
@@ -492,8 +497,8 @@ __global__ __launch_bounds__(256, 2) void qattn_few_kernel(QAttnArgs a) {
         if (left < kQTokens && (t >> 1) * 32 + lq * 8 + (t & 1) * 4 + e >= left) s[t][e] = -INFINITY;
         m = fmaxf(m, s[t][e]);
       }
-    m = fmaxf(m, __shfl_xor(m, 16, 64));
-    m = half_swap_max(m);
+    const auto other = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    m = half_swap_max(fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1])));
     m = fmaxf(m + kHeadroom, ref);
     const float m0 = m == -INFINITY ? 0.0f : m, f = __builtin_amdgcn_exp2f(ref - m0);
     ref = m;
@@ -517,7 +522,7 @@ __global__ __launch_bounds__(256, 2) void qattn_few_kernel(QAttnArgs a) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
     if (i + STAGES < n) issue(slot, i + STAGES);
     slot ^= 1;
-    if (((i + 1) & 63) == 0 && i + 1 < n) sc = scales[4 * min(i + 1 + lane, n - 1)];
+    if (((i + 1) & 63) == 0 && i + 1 < n) sc = scales[W * min(i + 1 + lane, n - 1)];
   }
   // joined: query r's dims of wave w at lds + (w * 16 + r) * 76 floats
   constexpr int LD = D + 4;
@@ -532,15 +537,15 @@ __global__ __launch_bounds__(256, 2) void qattn_few_kernel(QAttnArgs a) {
   }
   __syncthreads();
   const int nq = min(16, r1 - q0);
-  for (int c = tid; c < nq * (D / 4); c += 256) {
+  for (int c = tid; c < nq * (D / 4); c += 64 * W) {
     const int q = c / (D / 4), dim = (c - q * (D / 4)) * 4;
     float M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, wave_m[w][q]);
+    for (int w = 0; w < W; ++w) M = fmaxf(M, wave_m[w][q]);
     f32x4 num = zero4;
     float den = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float f = M == -INFINITY ? 1.0f : exp2f(wave_m[w][q] - M);  // (no maximum: sums are 0, or NaN)
       const f32x4 v = *(const f32x4 *)(res + (w * 16 + q) * LD + dim);
 #pragma unroll
@@ -601,11 +606,10 @@ __global__ __launch_bounds__(64) void qattn_combine_kernel(QAttnArgs a) {
 // Kernel and key splits: the pair with the least estimated time.  A tile of 64
 // keys takes a CU's two workgroups 1.45 us at QH = 1 and 2.3 at QH = 2, a lone
 // one 0.7 and 0.6 of that; the ends 6 and 8 us; a combine 4 us and its bytes at
-// about 4 TB/s.  Of the kernel for few queries a wave takes a tile in 1.35 us,
-// 1.75 with two workgroups on its CU, and the cache's bytes at most 5.5 TB/s;
-// its ends take 5.5 us.  Best of each with its combine, us (few, QH = 1, QH = 2):
-// one query of 16384 keys 17.0, 26.5; one of 4096 10.4, 13.7; 64 of 4096 14.5,
-// 16.2; 128 of 4096 17.9, 19.7; 154 of 1024 QH = 1 14.6, QH = 2 16.6; 723 of 4096
+// about 4 TB/s.  Of the kernel for few queries a wave takes a tile in 1.75 us and
+// the cache's bytes at most 5.5 TB/s; its ends take 5.5 us.  Best of each with
+// its combine, us (few, QH = 1, QH = 2): one query of 16384 keys 15.6, 26.5; one of
+// 4096 10.1, 13.7; 64 of 4096 13.3, 16.2; 128 of 4096 16.7, 19.7; 154 of 1024 QH = 1 14.6, QH = 2 16.6; 723 of 4096
 // 36.8 (five splits) and 39.0; 1639 61.1 and 57.5; 4096 97.0 and 98.0; 1639 of
 // 16384 175 and 160; 16384 of 16384 1412 and 1204.
 QAttnPlan plan_qattention(const int *offsets, int chains, int heads, int tokens) {
@@ -627,7 +631,7 @@ QAttnPlan plan_qattention(const int *offsets, int chains, int heads, int tokens)
       const double wgs = (double)qtiles * heads * sp, tiles = (n_tiles + sp - 1) / sp;
       double us = sp > 1 ? 4.0 + rows * heads * kHeadDim * 4.0 * (sp + 1) / 4e6 : 0.0;
       if (qh == 0)
-        us += 5.5 + std::max((wgs <= 256 ? 1.35 : 1.75 * std::ceil(wgs / 512)) * std::ceil(tiles / 4),
+        us += 5.5 + std::max(1.75 * std::ceil(wgs / 256) * std::ceil(tiles / kFewWaves),
                              full * heads * (double)tokens * 2 * kHeadDim / 5.5e6);
       else
         us += (qh == 1 ? 6.0 : 8.0) +
@@ -649,7 +653,7 @@ hipError_t launch_qattention(const QAttnArgs &args, int chains, const QAttnPlan 
   if (std::fabs(a.scale_log2) < 1e-30f) a.scale_log2 = 1e-30f;
   a.chains = chains;
   const dim3 grid((unsigned)p.workgroups);
-  if (p.qh == 0) rc_launch(qattn_few_kernel, grid, dim3(256), 0, s, a);
+  if (p.qh == 0) rc_launch(qattn_few_kernel, grid, dim3(64 * kFewWaves), 0, s, a);
   else if (p.qh == 2) rc_launch(qattn_kernel<2>, grid, dim3(256), 0, s, a);
   else rc_launch(qattn_kernel<1>, grid, dim3(256), 0, s, a);
   return hipGetLastError();

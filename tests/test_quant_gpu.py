@@ -193,6 +193,7 @@ def test_qgemm_large(Q, m, n, k, ldo):
         check_product(buf[:m, :n], a, ea, w, ew, bias, gelu, False)
     Q.qgemm(A, W, out=buf[:m, :n])
     check_product(buf[:m, :n], a, ea, w, ew, None, False, False)
+    assert torch.equal(Q.qgemm(A, W), buf[:m, :n])  # (the same again)
     assert (buf[:, n:] == 77.0).all() and (buf[m:] == 77.0).all()
 
 
@@ -532,6 +533,58 @@ def test_two_streams_at_once(Q):
     torch.cuda.synchronize()
     for g, w in zip(got, want):
         assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
+
+
+# ------------------------------------------------------------------ offsets beyond 32 bits
+
+def test_quantize_beyond_32_bits(Q):
+    """4.3e9 values: the last row, and the block before the last of a tile."""
+    rows, cols = 1 << 18, 16384
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    last = rnd(torch.bfloat16, 1, cols, seed=3)
+    x[-1] = dev(last, torch.bfloat16)[0]
+    for tile in (1, 128):
+        m = Q.quantize(x, tile)
+        block = np.zeros((128, cols))
+        block[-1] = last[0]
+        q, e = R.quantize(block, tile)
+        np.testing.assert_array_equal(codes(m.data[-128:]), q)
+        used = rows // tile
+        np.testing.assert_array_equal(m.scales[:, used - 128 // tile:used].cpu().numpy(), e)
+        assert (m.data[:-1].view(torch.int64) == 0).all()
+        del m
+
+
+def test_qgemm_beyond_32_bits(Q):
+    """2.4e9 results, of two steps of K per tile."""
+    m, n, k = 40000, 60001 // 8 * 8, 256
+    a, ea, w, ew = product(m, n, k, seed=21)
+    y = Q.qgemm(matrix(Q, a, ea, 1), matrix(Q, w, ew, 128))
+    rows = np.concatenate([[0, 255, 256, m - 1], np.random.default_rng(1).integers(0, m, 20)])
+    check_product(y[torch.from_numpy(rows).cuda()], a[rows], ea[:, rows], w, ew, None, False, False)
+    assert torch.isfinite(y.view(-1)[::7].float()).all()
+
+
+def test_cache_beyond_32_bits(Q):
+    """A cache of 4.8 GB, zeros but for its last block: its keys' weight is 1 each, the last ones' about e^14."""
+    heads, tokens = 2, 1 << 24
+    cache = Q.QuantCache.alloc(1, heads, tokens)
+    per = [list(range(tokens - 64, tokens))]
+    q = rnd(torch.bfloat16, 1, heads * 72, seed=1)
+    unit = q.reshape(heads, 72) / (q.reshape(heads, 72) ** 2).sum(1, keepdims=True)
+    k = np.repeat((unit * 14.0 * 72 ** 0.5).reshape(1, -1), 64, 0) * np.linspace(0.9, 1.0, 64)[:, None]
+    v = rnd(torch.bfloat16, 64, heads * 72, seed=2)
+    Q.qcache_store(cache, active(per), dev(k, torch.bfloat16), dev(v, torch.bfloat16))
+    o = np64(Q.qcache_attention(cache, rows_set([1]), dev(q, torch.bfloat16)))
+    assert (cache.data[0, :, :-1, :, 0].view(torch.uint8) == 0).all()
+    K, V = (codes(cache.data[0, :, -1, i]) * 2.0 ** (cache.scales[0, :, -1, i].cpu().numpy().astype(float) - 127)[:, None, None]
+            for i in (0, 1))
+    p = np.exp(72 ** -0.5 * np.einsum("htd,hd->ht", K, q.reshape(heads, 72)))
+    den = p.sum(1) + (tokens - 64)
+    ref, mean_abs = (np.einsum("ht,htd->hd", p, x) / den[:, None] for x in (V, np.abs(V)))
+    # the probabilities and the result rounded, 2^-9 each; sums of 4096 steps per wave, 2^-12
+    tol = 2.0 ** -8 * (2 * np.abs(ref) + mean_abs) + 2.0 ** -12 * mean_abs
+    assert (np.abs(o.reshape(heads, 72) - ref) <= tol).all()
 
 
 def test_empty_calls(Q):

@@ -47,19 +47,28 @@ template <int N> __device__ __forceinline__ void wait_vm8() { asm volatile("s_wa
 __device__ __forceinline__ void lds_barrier8() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // This workgroup's chain, head, key range and query rows q0 .. (at most bq, up
-// to r1); false if it has none.  Heads and key ranges are outermost, so that
-// every XCD has a share of every chain, however ragged the chains' rows and
-// keys are, and the query tiles that read the same keys are on one XCD (by
-// chains, six of 0..655 rows took 109 us, with one XCD in two idle, now 50).
+// to r1); false if it has none.  Heads and key ranges are shared out to the
+// XCDs, so that each has a part of every chain, however ragged the chains' rows
+// and keys are, and the query tiles that read the same keys are on one XCD.
+// Within an XCD the query tiles are outermost, so that a long chain's are on
+// different CUs.  (Six chains of 0..655 rows and 0..4096 keys 44 us; heads
+// outermost 54, a busy tile on every eighth CU; chains outermost 109.)
 // The grid holds the query tiles of all chains, or for more chains than the
 // arguments hold the longest one's for each.
 __device__ __forceinline__ bool locate(const QAttnArgs &a, int bq, int &b, int &h, int &split, int &q0, int &r1) {
-  const int tiles_q = gridDim.x / (a.c.heads * a.splits);
-  const int L = xcd_logical_id(blockIdx.x, gridDim.x);
-  const int hy = L / tiles_q;
+  const int n_hs = a.c.heads * a.splits, tiles_q = gridDim.x / n_hs;
+  int hy, qt;
+  if ((n_hs & 7) == 0) {  // an XCD's share in order of query tiles
+    const int x = blockIdx.x & 7, i = blockIdx.x >> 3, per = n_hs >> 3;
+    qt = i / per;
+    hy = x * per + i - qt * per;
+  } else {
+    const int L = xcd_logical_id(blockIdx.x, gridDim.x);
+    hy = L / tiles_q;
+    qt = L - hy * tiles_q;
+  }
   h = hy % a.c.heads;
   split = hy / a.c.heads;
-  int qt = L - hy * tiles_q;
   b = 0;
   if (a.chains <= kQArgChains) {
     for (; b < a.chains - 1; ++b) {

@@ -510,14 +510,15 @@ template <int PLACE> __device__ __forceinline__ void lds_copy16(const void *from
 // wave (all 256 accumulation registers): a step of K, 64 matrix instructions or
 // 2048 clocks, takes 32 KB of fragments a wave and 64 KB of copies from memory,
 // where 128 x 128 tiles of 64 x 64 per wave take all that LDS gives and twice
-// the copies.  With one wave per SIMD nothing but the order of instructions
-// covers latency:
+// the copies.  (FM = 6: 192 x 256, three quarters of the work in 0.86 of the time,
+// where that saves a part of a round of workgroups.)  With one wave per SIMD
+// nothing but the order of instructions covers latency:
 // * stages of 128 of K in a ring of two.  A step's first half multiplies column
 //   by column and reads the rest of its W fragments at once; then the stage is
 //   in registers and its place takes the stage after next.  The second half
 //   multiplies row by row and reads the next stage's fragments into the
 //   registers of the rows that are done with.
-// * Copies are issued one between two products, every third product (all at
+// * Copies are issued one between two products, every second or third (all at
 //   once they hold a wave up for 1100 clocks a step; with a branch each, 400).
 // * The steps of a workgroup's tiles are one sequence: the last two steps of a
 //   tile copy the next one's first stages, which arrive during the epilogue.
@@ -527,24 +528,25 @@ template <int PLACE> __device__ __forceinline__ void lds_copy16(const void *from
 // 21000 at K = 1152, and nothing covers it (accumulators of a second tile find
 // no registers).  16384 x 4608 x 1152: 99 us (128 x 128 tiles 118), 104 with GELU
 // (134); 8192 x 8192 x 9216: 462 us, 2.7 PFLOP/s.
-template <int EPI>
+template <int FM, int EPI>
 __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int tiles) {
-  constexpr int B = 256, F = 8, HALF = B * kQBlock, STAGE = 2 * HALF, NC = HALF / 4096;
+  constexpr int FN = 8, BM = 32 * FM, BN = 32 * FN, W0 = BM * kQBlock, STAGE = W0 + BN * kQBlock;
+  constexpr int NA = FM, NW = FN;  // copies of a stage: rows, W
   constexpr bool GELU = EPI == QG_GELU || EPI == QG_GELU8;
   // per slot: rows, W; behind the ring, per slot: the rows' scales, W's four; for two tiles: the bias
-  constexpr int SCALES = 2 * STAGE, BIAS = SCALES + 2 * 2 * B;
-  __shared__ __attribute__((aligned(1024))) char lds[BIAS + 2 * 4 * B];
+  constexpr int SCALES = 2 * STAGE, BIAS = SCALES + 2 * 512;
+  __shared__ __attribute__((aligned(1024))) char lds[BIAS + 2 * 4 * BN];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   __builtin_assume(wave >= 0 && wave < 4);
   const int wm = wave >> 1, wn = wave & 1, l16 = lane & 15, lq = lane >> 4;
-  const int tiles_m = (g.M + B - 1) / B, tiles_n = (g.N + B - 1) / B, n = g.K / kQBlock;
+  const int tiles_m = (g.M + BM - 1) / BM, tiles_n = (g.N + BN - 1) / BN, n = g.K / kQBlock;
   // bands of GM row tiles, as above
-  constexpr int GM = 2048 / B;
+  constexpr int GM = 2048 / BM;
   auto place = [&](int p, int &m0, int &n0) {
     const int L = xcd_logical_id(p, tiles);
     const int band0 = L / (GM * tiles_n), gm = min(GM, tiles_m - band0 * GM), idx = L - band0 * GM * tiles_n;
-    m0 = __builtin_amdgcn_readfirstlane((band0 * GM + idx % gm) * B);
-    n0 = __builtin_amdgcn_readfirstlane(idx / gm * B);
+    m0 = __builtin_amdgcn_readfirstlane((band0 * GM + idx % gm) * BM);
+    n0 = __builtin_amdgcn_readfirstlane(idx / gm * BN);
   };
 
   const unsigned ring0 = __builtin_amdgcn_readfirstlane(lds_address(lds)), mine = ring0 + wave * 1024;
@@ -552,7 +554,7 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
   // The next stage to be copied: rows, W, their scales.
   const int row8 = wave * 8 + (lane >> 3), chunk = ((lane & 7) ^ ((row8 >> 1) & 7)) * 16;
   const uint8_t *c_a, *c_w, *c_as, *c_ws;
-  unsigned off_a[NC], off_w[NC];
+  unsigned off_a[NA], off_w[NW];
   int c_rows, by = kQBlock, as_by = g.as_ld, ws_by = g.ws_ld;
   auto enter = [&](int m0, int n0) {  // a tile's first
     c_a = g.a + m0 * g.lda;
@@ -560,14 +562,14 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
     c_as = g.as + m0;
     c_ws = g.ws + (n0 / kQBlock & ~3);
     c_rows = g.M - 1 - m0;
+    // (rows behind the last are copies of it)
 #pragma unroll
-    for (int q = 0; q < NC; ++q) {  // (rows behind the last are copies of it)
-      off_a[q] = __umul24((unsigned)min(row8 + q * 32, c_rows), (unsigned)g.lda) + chunk;
-      off_w[q] = __umul24((unsigned)min(row8 + q * 32, g.N - 1 - n0), (unsigned)g.ldw) + chunk;
-    }
+    for (int q = 0; q < NA; ++q) off_a[q] = __umul24((unsigned)min(row8 + q * 32, c_rows), (unsigned)g.lda) + chunk;
+#pragma unroll
+    for (int q = 0; q < NW; ++q) off_w[q] = __umul24((unsigned)min(row8 + q * 32, g.N - 1 - n0), (unsigned)g.ldw) + chunk;
   };
   auto copy_bias = [&](int n0, int which) {  // (a wave's 64 columns)
-    lds_dma4s(g.bias, (unsigned)min(n0 + wave * 64 + lane, g.N - 1) * 4u, ring0 + BIAS + which * 4 * B + wave * 256);
+    lds_dma4s(g.bias, (unsigned)min(n0 + wave * 64 + lane, g.N - 1) * 4u, ring0 + BIAS + which * 4 * BN + wave * 256);
   };
   auto advance = [&]() {
     c_a += by;
@@ -577,38 +579,37 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
   };
   // (the same by every wave, so that every wave has the same copies in flight)
   auto copy_scales = [&](int slot) {
-    const unsigned to = ring0 + SCALES + slot * 2 * B;
+    const unsigned to = ring0 + SCALES + slot * 512;
     lds_dma4s(c_as, (unsigned)min(lane * 4, c_rows & ~3), to);
-    lds_dma4s(c_ws, 0, to + B);
+    lds_dma4s(c_ws, 0, to + 256);
   };
-  auto copy_a = [&](int slot, int q) {
-    switch (q) {
-#define RC_CASE(Q) case Q: return lds_copy16<Q * 4096>(c_a, off_a[Q], mine + slot * STAGE);
+  auto copy = [&](int slot, int c) {  // the rows' copies, then W's
+    switch (c) {
+#define RC_CASE(Q) \
+  case Q: return lds_copy16<Q * 4096>(Q < NA ? c_a : c_w, Q < NA ? off_a[Q < NA ? Q : 0] : off_w[Q < NA ? 0 : Q - NA], mine + slot * STAGE);
       RC_CASE(0) RC_CASE(1) RC_CASE(2) RC_CASE(3) RC_CASE(4) RC_CASE(5) RC_CASE(6) RC_CASE(7)
+      RC_CASE(8) RC_CASE(9) RC_CASE(10) RC_CASE(11) RC_CASE(12) RC_CASE(13)
 #undef RC_CASE
     }
-  };
-  auto copy_w = [&](int slot, int q) {
-    switch (q) {
-#define RC_CASE(Q) case Q: return lds_copy16<HALF + Q * 4096>(c_w, off_w[Q], mine + slot * STAGE);
-      RC_CASE(0) RC_CASE(1) RC_CASE(2) RC_CASE(3) RC_CASE(4) RC_CASE(5) RC_CASE(6) RC_CASE(7)
-#undef RC_CASE
+    if constexpr (NA + NW == 16) {
+      if (c == 14) lds_copy16<14 * 4096>(c_w, off_w[NW - 2], mine + slot * STAGE);
+      if (c == 15) lds_copy16<15 * 4096>(c_w, off_w[NW - 1], mine + slot * STAGE);
     }
   };
 
-  f32x4 acc[F][F];
+  f32x4 acc[FM][FN];
   const int sz = (l16 >> 1) & 7, c_lo = l16 * kQBlock + ((lq ^ sz) << 4), c_hi = l16 * kQBlock + (((lq + 4) ^ sz) << 4);
-  i32x8 a[F], w[F];
-  int ea[F], ew, ew_next;
+  i32x8 a[FM], w[FN];
+  int ea[FM], ew, ew_next;
   auto frag = [&](const char *rows) {
     return __builtin_shufflevector(*(const i32x4 *)(rows + c_lo), *(const i32x4 *)(rows + c_hi), 0, 1, 2, 3, 4, 5, 6, 7);
   };
   auto read_a = [&](int slot, int i) {
-    a[i] = frag(lds + slot * STAGE + (wm * F + i) * 16 * kQBlock);
-    ea[i] = *(const uint8_t *)(lds + SCALES + slot * 2 * B + (wm * F + i) * 16 + l16);
+    a[i] = frag(lds + slot * STAGE + (wm * FM + i) * 16 * kQBlock);
+    ea[i] = *(const uint8_t *)(lds + SCALES + slot * 512 + (wm * FM + i) * 16 + l16);
   };
-  auto read_w = [&](int slot, int j) { w[j] = frag(lds + slot * STAGE + HALF + (wn * F + j) * 16 * kQBlock); };
-  auto read_ew = [&](int slot, int byte) { return (int)*(const uint8_t *)(lds + SCALES + slot * 2 * B + B + byte); };
+  auto read_w = [&](int slot, int j) { w[j] = frag(lds + slot * STAGE + W0 + (wn * FN + j) * 16 * kQBlock); };
+  auto read_ew = [&](int slot, int byte) { return (int)*(const uint8_t *)(lds + SCALES + slot * 512 + 256 + byte); };
 
   int m0, n0;
   place(blockIdx.x, m0, n0);
@@ -619,51 +620,46 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
   for (int s = 0; s < 2; ++s) {
     copy_scales(s);
 #pragma unroll
-    for (int q = 0; q < NC; ++q) copy_a(s, q);
-#pragma unroll
-    for (int q = 0; q < NC; ++q) copy_w(s, q);
+    for (int c = 0; c < NA + NW; ++c) copy(s, c);
     advance();
   }
-  wait_vm_q<2 + 2 * NC>();
+  wait_vm_q<2 + NA + NW>();
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   ew = read_ew(0, (n0 / kQBlock & 3) + wn);
 #pragma unroll
-  for (int j = 0; j < F / 2; ++j) read_w(0, j);
+  for (int j = 0; j < FN / 2; ++j) read_w(0, j);
 #pragma unroll
-  for (int i = 0; i < F; ++i) read_a(0, i);
+  for (int i = 0; i < FM; ++i) read_a(0, i);
 
   int slot = 0, which = 0;
   auto multiply = [&](int q, int j) {
     acc[q][j] = q_mma<false>(w[j], a[q], acc[q][j], ew, ea[q]);
     asm volatile("" : "+a"(acc[q][j]));  // (in its place)
   };
-  constexpr int FROM = 13, EVERY = 3;  // products before the first copy, and between two
+  constexpr int HALF = FM * FN / 2, FROM = 13, EVERY = FM == 8 ? 3 : 2;  // products before the first copy, and between two
+  static_assert(FROM + EVERY * (NA + NW - 1) < 2 * HALF, "a step issues all copies of a stage");
   auto step = [&](int byte) {  // byte: W's scale of the next stage
 #pragma unroll
-    for (int t8 = 0; t8 < F; ++t8)
+    for (int t8 = 0; t8 < FM; ++t8)
 #pragma unroll
-    for (int t1 = 0; t1 < F; ++t1) {
-      const int t = t8 * F + t1;
-      // the first half column by column, the second row by row
-      const int q = t < 32 ? t % F : (t - 32) / 4, j = t < 32 ? t / F : 4 + t % 4;
-      multiply(q, j);
-      if (t < 4) read_w(slot, 4 + t);
-      if (t == 11) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // every wave has all of this stage
-      if (t == 12) copy_scales(slot);
-      if (t >= FROM && t < FROM + EVERY * 2 * NC && (t - FROM) % EVERY == 0) {
-        const int c = (t - FROM) / EVERY;
-        if (c < NC) copy_a(slot, c);
-        else copy_w(slot, c - NC);
+      for (int t1 = 0; t1 < FN; ++t1) {
+        const int t = t8 * FN + t1;
+        // the first half column by column, the second row by row
+        const int q = t < HALF ? t % FM : (t - HALF) / 4, j = t < HALF ? t / FM : 4 + t % 4;
+        multiply(q, j);
+        if (t < 4) read_w(slot, 4 + t);
+        if (t == 11) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // every wave has all of this stage
+        if (t == 12) copy_scales(slot);
+        if (t >= FROM && (t - FROM) % EVERY == 0 && (t - FROM) / EVERY < NA + NW) copy(slot, (t - FROM) / EVERY);
+        if (t == HALF - 1) {  // the next stage is there
+          wait_vm_q<2 + (HALF - FROM + EVERY - 1) / EVERY>();
+          asm volatile("s_barrier" ::: "memory");
+        }
+        if (t >= HALF && (t - HALF) % FM == 1) read_w(slot ^ 1, (t - HALF) / FM);
+        if (t == 2 * HALF - 11) ew_next = read_ew(slot ^ 1, byte);
+        if (t >= HALF && j == 7) read_a(slot ^ 1, q);  // (behind the last stage: stale, never used)
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if (t == 31) {  // the next stage is there
-        wait_vm_q<2 + (32 - FROM + EVERY - 1) / EVERY>();
-        asm volatile("s_barrier" ::: "memory");
-      }
-      if (t >= 32 && t % 8 == 1) read_w(slot ^ 1, (t - 32) / 8);
-      if (t == 53) ew_next = read_ew(slot ^ 1, byte);
-      if (t >= 32 && j == 7) read_a(slot ^ 1, q);  // (behind the last stage: stale, never used)
-      __builtin_amdgcn_sched_barrier(0);
-    }
     ew = ew_next;
     advance();
     slot ^= 1;
@@ -675,9 +671,9 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
     if (t + (int)gridDim.x < tiles) place(t + gridDim.x, next_m0, next_n0);
     const int byte = (n0 / kQBlock & 3) + wn, next_byte = (next_n0 / kQBlock & 3) + wn;
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int j = 0; j < F; ++j) {
+      for (int j = 0; j < FN; ++j) {
         acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         asm volatile("" : "+a"(acc[i][j]));
       }
@@ -704,16 +700,16 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
     // lane (l16, lq) holds, of row i * 16 + l16, columns j * 16 + lq * 4 .. + 3
     int my = lane;
     asm volatile("" : "+v"(my));  // (nothing that follows is made ahead and kept)
-    const int lq = my >> 4, col0 = n0 + wn * 128, row0 = m0 + wm * 128 + (my & 15);
-    const char *bias_at = lds + BIAS + which * 4 * B + (wn * 128 + lq * 4) * 4;
+    const int lq = my >> 4, col0 = n0 + wn * 128, row0 = m0 + wm * (16 * FM) + (my & 15);
+    const char *bias_at = lds + BIAS + which * 4 * BN + (wn * 128 + lq * 4) * 4;
     m0 = next_m0;
     n0 = next_n0;
     which ^= 1;
     if constexpr (EPI == QG_RESID) {
       // half a row block of 16 at a time, its X and place loaded one half ahead
       // (rows and columns behind the last: any valid ones)
-      constexpr int H = F / 2;
-      f32x4 gate[F], x[2][H];
+      constexpr int H = FN / 2;
+      f32x4 gate[FN], x[2][H];
       int packed[2];
       auto load = [&](int u) {
         const int row = min(row0 + u / 2 * 16, g.M - 1);
@@ -723,18 +719,18 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
           x[u & 1][j] = *(const f32x4 *)(g.X + (size_t)row * g.N + min(col0 + (u % 2 * H + j) * 16 + lq * 4, g.N - 4));
       };
 #pragma unroll
-      for (int j = 0; j < F; ++j) {
+      for (int j = 0; j < FN; ++j) {
         const int col = min(col0 + j * 16 + lq * 4, g.N - 4);
         gate[j] = *(const f32x4 *)(g.gate + col) + *(const f32x4 *)(g.gate2 + col);
       }
       load(0);
 #pragma unroll
-      for (int i = 0; i < F; ++i)
+      for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const int u = i * 2 + half, row = row0 + i * 16;
           __builtin_amdgcn_sched_barrier(0);
-          if (u + 1 < 2 * F) load(u + 1);
+          if (u + 1 < 2 * FM) load(u + 1);
           bf16 *h = g.hslot + row_chain(packed[u & 1]) * g.chain_stride + (size_t)row_token(packed[u & 1]) * g.N;
 #pragma unroll
           for (int j = half * H; j < half * H + H; j += 2) {
@@ -757,15 +753,15 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
           }
         }
     } else {
-      f32x4 bias[F];
+      f32x4 bias[FN];
 #pragma unroll
-      for (int j = 0; j < F; ++j) bias[j] = *(const f32x4 *)(bias_at + j * 64);
+      for (int j = 0; j < FN; ++j) bias[j] = *(const f32x4 *)(bias_at + j * 64);
 #pragma unroll
-      for (int i = 0; i < F; ++i) {
+      for (int i = 0; i < FM; ++i) {
         const int row = row0 + i * 16;
-        float v[F][4];
+        float v[FN][4];
 #pragma unroll
-        for (int j = 0; j < F; ++j) {
+        for (int j = 0; j < FN; ++j) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             v[j][e] = acc[i][j][e] + bias[j][e];
@@ -775,7 +771,7 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
         if constexpr (EPI == QG_GELU8) {
           float m = 0.0f;
 #pragma unroll
-          for (int j = 0; j < F; ++j)
+          for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) m = fmaxf(m, q_magnitude(v[j][e]));
           uint32_t m0_ = __float_as_uint(m), m1_ = m0_;
@@ -784,7 +780,7 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
           const int ex = q_exponent(m);
           const float inv = q_inverse(ex);
 #pragma unroll
-          for (int h = 0; h < F; h += 4) {  // four blocks of 16 columns: lane group lq gets block h + lq
+          for (int h = 0; h < FN; h += 4) {  // four blocks of 16 columns: lane group lq gets block h + lq
             uint32_t d[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) d[k] = q_pack4(v[h + k], inv);
@@ -798,7 +794,7 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
           if (lq == 0 && row < g.M && col0 < g.N) g.out_scales[(size_t)(col0 / kQBlock) * g.out_scale_ld + row] = (uint8_t)ex;
         } else {
 #pragma unroll
-          for (int j = 0; j < F; j += 2) {  // two blocks of 16 columns: eight in a row for each lane
+          for (int j = 0; j < FN; j += 2) {  // two blocks of 16 columns: eight in a row for each lane
             uint32_t u[2][2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -838,9 +834,11 @@ template <int EPI, typename OUT> static hipError_t launch_qg(const QGemmArgs &a,
   if (tile == 64128) RC_QG(4, 2, 1, 4, 1, 3);
   if (tile == 128128) RC_QG(4, 4, 2, 2, 1, 2);
   if constexpr (sizeof(OUT) == 2)
-    if (tile == 256256) {
+    if (p.bn == 256) {
       if (a.K % kQBlock || a.K < 2 * kQBlock || a.N % 8 || a.ldo % 8) return hipErrorInvalidValue;
-      return rc_launch(qgemm_large_kernel<EPI>, dim3(std::min(tiles, 256u)), dim3(256), 0, s, a, (int)tiles);
+      const dim3 grid(std::min(tiles, 256u));
+      if (p.bm == 192) return rc_launch(qgemm_large_kernel<6, EPI>, grid, dim3(256), 0, s, a, (int)tiles);
+      if (p.bm == 256) return rc_launch(qgemm_large_kernel<8, EPI>, grid, dim3(256), 0, s, a, (int)tiles);
     }
 #undef RC_QG
 #undef RC_QG_SPLIT
@@ -853,15 +851,16 @@ template <int EPI, typename OUT> static hipError_t launch_qg(const QGemmArgs &a,
 // Measured, us (kernels alone): 16 x 16, 32 x 32, 64 x 32 and 64 x 64 tiles 1 x 4608 x
 // 1152 4.6, 4.6, 6.0, 7.2; 16 x 1152 x 4608 7.4, 9.6, 10.4, 13.0; 64 x 4608 x 1152 8.7, 7.3,
 // 6.0, 7.4; 200 x 1152 x 640 5.9, 4.4, 5.4, 6.5; 200 x 1152 x 4608 19.7, 12.0, 11.4, 13.6;
-// 723 x 1152 x 4608 -, -, 21, 15.  With launches, 64 x 128, 128 x 128 and 256 x 256:
-// 723 x 4608 x 1152 13.3, 14.9, -; 1639 x 4608 x 1152 22.5, 16.4, 21.2; 2401 x 4608 x 1152
-// 32, 25.9, 22.1; 3500 x 1152 x 4608 31.1, 31.4, 44.2; 4096 x 4608 x 1152 -, 38, 41 (288
-// tiles for 256 CUs); 5800 x 1152 x 4608 56, 38, 46; 8192 x 1152 x 4608 77, 65, 49;
-// 16384 x 4608 x 1152 -, 118, 99.
+// 723 x 1152 x 4608 -, -, 21, 15.  With launches, 64 x 128, 128 x 128, 192 x 256 and 256
+// x 256: 723 x 4608 x 1152 13.3, 14.9, -, -; 1639 x 4608 x 1152 22.5, 16.4, 18.6, 21.0;
+// 2401 x 4608 x 1152 31.5, 26.2, 19.7, 22.1; 3500 x 4608 x 1152 42, 31, 34, 24.8 (342 and
+// 252 of the large tiles for 256 CUs); 3500 x 1152 x 4608 30.9, 31.5, 38.8, 43.7; 4096 x
+// 4608 x 1152 48, 39, 35, 41; 8192 x 1152 x 4608 76, 66, 46.7, 48.9; 16384 x 4608 x 1152 171,
+// 132, 119, 107; 16384 x 1152 x 4608 146, 121, 90, 100.
 QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi, bool large) {
   struct Tile { int bm, bn, kg; double per, end; };  // us a step, a tile
   static constexpr Tile tiles[] = {{16, 16, 8, 1.0, 0.0}, {32, 32, 8, 1.7, 0.0}, {64, 32, 4, 0.65, 1.2}, {64, 64, 4, 0.85, 1.9},
-                                   {64, 128, 1, 0.33, 0.6}, {128, 128, 1, 0.44, 1.0}, {256, 256, 0, 1.1, 6.5}};
+                                   {64, 128, 1, 0.33, 0.6}, {128, 128, 1, 0.44, 1.0}, {192, 256, 0, 1.0, 5.9}, {256, 256, 0, 1.1, 7.5}};
   const int blocks = (K + kQBlock - 1) / kQBlock;
   QGemmPlan best{128, 128};
   double best_us = 1e30;

@@ -179,7 +179,8 @@ def test_qgemm_nan_stays_in_its_row_and_column(Q, m, f32):
     np.testing.assert_array_equal(np.isnan(y), bad)
 
 
-LARGE = [(3001, 4360, 640, 4360), (4500, 6000, 384, 6016)]  # 256 x 256 tiles: one round of workgroups, two; the last in gaps
+# 256 x 256 tiles in one round of workgroups, 128 x 128, 256 x 256 in two rounds, 192 x 256 in one and two; some into gaps
+LARGE = [(3001, 4360, 640, 4360), (4500, 6000, 384, 6016), (5700, 5000, 640, 5016), (2300, 4600, 896, 4600), (4100, 4600, 1152, 4616)]
 
 
 @pytest.mark.parametrize("m,n,k,ldo", LARGE)
@@ -197,13 +198,13 @@ def test_qgemm_large(Q, m, n, k, ldo):
     assert (buf[:, n:] == 77.0).all() and (buf[m:] == 77.0).all()
 
 
-def test_qgemm_large_nan_stays_in_its_row_and_column(Q):
-    m, n, k, _ = LARGE[0]
+@pytest.mark.parametrize("m,n,k,_", [LARGE[0], LARGE[3]])
+def test_qgemm_large_nan_stays_in_its_row_and_column(Q, m, n, k, _):
     a, ea, w, ew = product(m, n, k, seed=6)
-    a[2, 100], a[3000, 639], w[33, 7], w[4359, 0] = np.nan, np.nan, np.nan, np.nan
+    a[2, 100], a[m - 1, k - 1], w[33, 7], w[n - 1, 0] = np.nan, np.nan, np.nan, np.nan
     y = Q.qgemm(matrix(Q, a, ea, 1), matrix(Q, w, ew, 128))
     bad = torch.zeros(y.shape, dtype=torch.bool, device="cuda")
-    bad[[2, 3000]], bad[:, [33, 4359]] = True, True
+    bad[[2, m - 1]], bad[:, [33, n - 1]] = True, True
     assert torch.equal(torch.isnan(y), bad)
 
 

@@ -135,12 +135,13 @@ class QuantCache:
     __slots__ = ("_data", "_scales", "_struct", "batch", "heads", "tokens")
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor):
-        shape = data.shape
-        if data.dtype != _F8 or len(shape) != 6 or shape[3:] != (2, KEY_BLOCK, HEAD_DIM):
+        if data.dtype != _F8 or data.dim() != 6:
             raise ValueError(f"data must be float8_e4m3fn [batch, heads, blocks, 2, {KEY_BLOCK}, {HEAD_DIM}]")
-        if scales.dtype != _U8 or scales.shape != shape[:4]:
+        batch, heads, blocks, two, tokens, dim = data.shape
+        if two != 2 or tokens != KEY_BLOCK or dim != HEAD_DIM:
+            raise ValueError(f"data must be float8_e4m3fn [batch, heads, blocks, 2, {KEY_BLOCK}, {HEAD_DIM}]")
+        if scales.dtype != _U8 or scales.shape != (batch, heads, blocks, 2):
             raise ValueError("scales must be uint8 [batch, heads, blocks, 2]")
-        batch, heads, blocks = shape[:3]
         if not (batch and heads and blocks):
             raise ValueError("the cache is empty")
         if not (data.is_contiguous() or data[0].is_contiguous()) or not (scales.is_contiguous() or scales[0].is_contiguous()):

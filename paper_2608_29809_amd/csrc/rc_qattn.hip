@@ -614,14 +614,15 @@ __global__ __launch_bounds__(64) void qattn_combine_kernel(QAttnArgs a) {
 
 // Kernel and key splits: the pair with the least estimated time.  A tile of 64
 // keys takes a CU's two workgroups 1.45 us at QH = 1 and 2.3 at QH = 2, a lone
-// one 0.7 and 0.6 of that; the ends 6 and 8 us; a combine 4 us and its bytes at
-// about 4 TB/s.  Of the kernel for few queries a wave takes a tile in 1.75 us, a
-// workgroup's ends take 3, one after the other on a CU (33 queries of 16384 keys
-// in 5, 10 and 16 splits 21.1, 24.8 and 27.6), and the cache's bytes at most 5.5 TB/s.  Best of each with
-// its combine, us (few, QH = 1, QH = 2): one query of 16384 keys 15.6, 26.5; one of
-// 4096 10.1, 13.7; 64 of 4096 13.3, 16.2; 128 of 4096 16.7, 19.7; 154 of 1024 QH = 1 14.6, QH = 2 16.6; 723 of 4096
-// 36.8 (five splits) and 39.0; 1639 61.1 and 57.5; 4096 97.0 and 98.0; 1639 of
-// 16384 175 and 160; 16384 of 16384 1412 and 1204.
+// one 0.7 of that; the ends 6 us (8.5 for two) and 8; a combine 4 us and its bytes
+// at about 4 TB/s.  Of the kernel for few queries a wave takes a tile in 1.75 us,
+// a workgroup's ends take 3, one after the other on a CU (33 queries of 16384 keys
+// in 5, 10 and 16 splits 21.1, 24.8 and 27.6), and the cache's bytes at most 5.5
+// TB/s.  Best of each with its combine, us (few, QH = 1, QH = 2): one query of
+// 16384 keys 15.6, 26.5; one of 4096 10.1, 13.7; 64 of 4096 13.3, 16.2; 154 of 4096
+// 20.7, 24.5; 154 of 16384 QH = 1 39; 723 of 4096 36.8 (five splits) and 38.9; 1639 of
+// 4096 63.4 and 59.7; 4096 of 4096 98.2 and 101.9; 1639 of 16384 182 and 162; 16384 of
+// 16384 1398 and 1175.
 QAttnPlan plan_qattention(const int *offsets, int chains, int heads, int tokens) {
   const int n_tiles = tokens / kQTokens;
   const long long rows = offsets ? offsets[chains] : (long long)chains * tokens;
@@ -644,8 +645,8 @@ QAttnPlan plan_qattention(const int *offsets, int chains, int heads, int tokens)
         us += 2.5 + std::max(std::ceil(wgs / 256) * (3.0 + 1.75 * std::ceil(tiles / kFewWaves)),
                              3.0 + full * heads * (double)tokens * 2 * kHeadDim / 5.5e6);
       else
-        us += (qh == 1 ? 6.0 : 8.0) +
-              tiles * (qh == 1 ? 1.45 * (wgs <= 256 ? 0.7 : std::ceil(wgs / 512)) : 2.3 * (wgs <= 256 ? 0.6 : std::ceil(wgs / 512)));
+        us += (qh == 2 ? 8.0 : wgs <= 256 ? 6.0 : 8.5) +
+              tiles * (qh == 1 ? 1.45 : 2.3) * (wgs <= 256 ? 0.7 : std::ceil(wgs / 512));
       if (us < best_us) {
         best_us = us;
         best = QAttnPlan{qh, sp, grid * sp};

@@ -848,18 +848,20 @@ template <int EPI, typename OUT> static hipError_t launch_qg(const QGemmArgs &a,
 // The tile with the least estimated time: 5 us of ends, and for every tile that
 // a CU has to do a time for each step of K and an end.  Workgroups of small
 // tiles (kg 8) share a CU; those of kg 1 count as pairs where there are few.
-// Measured, us (kernels alone): 16 x 16, 32 x 32, 64 x 32 and 64 x 64 tiles 1 x 4608 x
-// 1152 4.6, 4.6, 6.0, 7.2; 16 x 1152 x 4608 7.4, 9.6, 10.4, 13.0; 64 x 4608 x 1152 8.7, 7.3,
-// 6.0, 7.4; 200 x 1152 x 640 5.9, 4.4, 5.4, 6.5; 200 x 1152 x 4608 19.7, 12.0, 11.4, 13.6;
-// 723 x 1152 x 4608 -, -, 21, 15.  With launches, 64 x 128, 128 x 128, 192 x 256 and 256
-// x 256: 723 x 4608 x 1152 13.3, 14.9, -, -; 1639 x 4608 x 1152 22.5, 16.4, 18.6, 21.0;
-// 2401 x 4608 x 1152 31.5, 26.2, 19.7, 22.1; 3500 x 4608 x 1152 42, 31, 34, 24.8 (342 and
-// 252 of the large tiles for 256 CUs); 3500 x 1152 x 4608 30.9, 31.5, 38.8, 43.7; 4096 x
-// 4608 x 1152 48, 39, 35, 41; 8192 x 1152 x 4608 76, 66, 46.7, 48.9; 16384 x 4608 x 1152 171,
-// 132, 119, 107; 16384 x 1152 x 4608 146, 121, 90, 100.
+// Measured, us (kernels alone): 16 x 16, 32 x 32, 64 x 32 and 64 x 64 tiles 1 x
+// 4608 x 1152 4.6, 4.6, 6.0, 7.2; 16 x 1152 x 4608 7.4, 9.6, 10.4, 13.0; 64 x 4608
+// x 1152 8.7, 7.3, 6.0, 7.4; 200 x 1152 x 640 5.9, 4.4, 5.4, 6.5; 200 x 1152 x
+// 4608 19.7, 12.0, 11.4, 13.6; 723 x 1152 x 4608 -, -, 21, 15 (64 x 128 24), 1517
+// x 1152 x 4608 -, -, 44, 31 (28).  With launches, 64 x 128, 128 x 128, 192 x 256
+// and 256 x 256: 723 x 4608 x 1152 13.3, 14.9, -, -; 1639 x 4608 x 1152 22.5,
+// 16.4, 18.6, 21.0; 2401 x 4608 x 1152 31.5, 26.2, 19.7, 22.1; 3500 x 4608 x 1152
+// 42, 31, 34, 24.8 (342 and 252 of the large tiles for 256 CUs); 3500 x 1152 x
+// 4608 30.9, 31.5, 38.8, 43.7; 4096 x 4608 x 1152 48, 39, 35, 41; 8192 x 1152 x
+// 4608 76, 66, 46.7, 48.9; 16384 x 4608 x 1152 171, 132, 119, 107; 16384 x 1152 x
+// 4608 146, 121, 90, 100.
 QGemmPlan plan_qgemm(int M, int N, int K, QGemmEpi epi, bool large) {
   struct Tile { int bm, bn, kg; double per, end; };  // us a step, a tile
-  static constexpr Tile tiles[] = {{16, 16, 8, 1.0, 0.0}, {32, 32, 8, 1.7, 0.0}, {64, 32, 4, 0.65, 1.2}, {64, 64, 4, 0.85, 1.9},
+  static constexpr Tile tiles[] = {{16, 16, 8, 1.0, 0.0}, {32, 32, 8, 1.7, 0.0}, {64, 32, 4, 0.65, 1.2}, {64, 64, 4, 1.0, 2.5},
                                    {64, 128, 1, 0.33, 0.6}, {128, 128, 1, 0.44, 1.0}, {192, 256, 0, 1.0, 5.9}, {256, 256, 0, 1.1, 7.5}};
   const int blocks = (K + kQBlock - 1) / kQBlock;
   QGemmPlan best{128, 128};

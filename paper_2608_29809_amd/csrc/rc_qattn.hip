@@ -423,7 +423,7 @@ template <int QH> __global__ __launch_bounds__(256, 2) void qattn_kernel(QAttnAr
 // and the waves' results are joined in LDS.  (Two workgroups of four waves on a
 // CU need twice the key splits: 64 queries of 4096 keys 14.0 instead of 13.3 us,
 // 33 of 16384 22.5 instead of 21.1.)  One query of 16384 keys: 15.6 us with its
-// combine, 38 MB or 7.4 us of the cache; 13 splits, in which a wave takes two or
+// combine, 38 MB or 7.4 us of the cache; 11 splits, in which a wave takes two or
 // three tiles, then the ends and the second launch.  16x16x32 blocks: rows m of two 16-key
 // operands are keys (m>>2)*8 + (m&3) and those + 4 of 32, so that a lane's
 // eight scores are those of the eight keys that PV takes from it.

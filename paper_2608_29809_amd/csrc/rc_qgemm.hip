@@ -614,8 +614,7 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
   int m0, n0;
   place(blockIdx.x, m0, n0);
   enter(m0, n0);
-  if (g.bias) copy_bias(n0, 0);
-  else *(f32x2 *)(lds + BIAS + tid * 8) = f32x2{0.0f, 0.0f};
+  if (!g.bias) *(f32x2 *)(lds + BIAS + tid * 8) = f32x2{0.0f, 0.0f};
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     copy_scales(s);
@@ -669,6 +668,10 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
   for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
     int next_m0 = m0, next_n0 = n0;
     if (t + (int)gridDim.x < tiles) place(t + gridDim.x, next_m0, next_n0);
+    // (the last tile's epilogue, in which another wave may still be, reads the
+    // other place; the one before it is over, a step's barriers ago.  The copy is
+    // older than the first step's, whose wait and barrier make it everybody's)
+    if (g.bias) copy_bias(n0, which);
     const int byte = (n0 / kQBlock & 3) + wn, next_byte = (next_n0 / kQBlock & 3) + wn;
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -686,7 +689,6 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
       if (i < n) {
         if (t + (int)gridDim.x < tiles) {
           enter(next_m0, next_n0);
-          if (g.bias) copy_bias(next_n0, which ^ 1);
         } else {  // no next one: the last stage again
           c_a -= by;
           c_w -= by;

@@ -177,7 +177,7 @@ class RegionCacheModel:
         ctx = C.c_void_p()
         abi.rc_create(C.byref(cfg), C.byref(w), C.byref(ctx))
         self.ctx = ctx
-        self._ws = None
+        self._ws = {}  # by the pool's bits
 
     def __del__(self):
         try:
@@ -217,10 +217,13 @@ class RegionCacheModel:
         return self._stage
 
     def workspace(self, max_rows: int, batch: int, bits: int = 16) -> torch.Tensor:
+        """The steps' workspace, one for each kind of pool, so that steps on
+        one never replace what a captured step on the other uses.  (More rows
+        than before do replace it: run the largest step before a capture.)"""
         nbytes = (abi.rc_quant_workspace_bytes if bits == 8 else abi.rc_workspace_bytes)(self.ctx, max_rows, batch)
-        if self._ws is None or self._ws.numel() < nbytes:
-            self._ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        return self._ws
+        if bits not in self._ws or self._ws[bits].numel() < nbytes:
+            self._ws[bits] = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return self._ws[bits]
 
     def to_storage(self, a) -> torch.Tensor:
         return torch.as_tensor(np.ascontiguousarray(a)).to(device=self.device, dtype=self.dtype)

@@ -178,6 +178,7 @@ class RegionCacheModel:
         abi.rc_create(C.byref(cfg), C.byref(w), C.byref(ctx))
         self.ctx = ctx
         self._ws = {}  # by the pool's bits
+        self._quant = None  # 8-bit weights, once made
 
     def __del__(self):
         try:
@@ -193,21 +194,26 @@ class RegionCacheModel:
 
     def quantize_weights(self, enable: bool = True):
         """Steps on an 8-bit pool take the QKV and MLP products from 8-bit
-        weights (made here, once), or with enable=False from the bf16 ones again."""
+        weights, or with enable=False from the bf16 ones again.  The 8-bit
+        weights are made here, in buffers that stay for later calls (which make
+        them anew, in place): a captured step may still read them."""
         from .quant import quantize
         if not enable:
             abi.rc_set_quant_weights(self.ctx, None)
-            torch.cuda.synchronize(self.device)  # (steps of any stream may still read them)
-            self._quant = None
             return
-        keep, layers = [], (abi.rc_quant_layer * self.L)()
-        for i, mats in enumerate(self._quantizable):
-            for f, t in mats.items():
-                keep.append(quantize(t, 128))
-                setattr(layers[i], f, keep[-1].struct())
+        if self._quant is None:
+            self._quant = [{f: quantize(t, 128) for f, t in mats.items()} for mats in self._quantizable]
+        else:
+            torch.cuda.synchronize(self.device)  # (steps of other streams may still read them)
+            for kept, mats in zip(self._quant, self._quantizable):
+                for f, t in mats.items():
+                    quantize(t, 128, kept[f])
+        layers = (abi.rc_quant_layer * self.L)()
+        for layer, kept in zip(layers, self._quant):
+            for f, q in kept.items():
+                setattr(layer, f, q.struct())
         abi.rc_set_quant_weights(self.ctx, layers)
-        torch.cuda.synchronize(self.device)  # (steps of other streams read them; earlier ones those that they replace)
-        self._quant = keep
+        torch.cuda.synchronize(self.device)  # (steps of other streams read them)
 
     def staging(self, batch: int) -> torch.Tensor:
         """Device staging ring of the host-resident pool."""

@@ -13,7 +13,7 @@ def model(monkeypatch):
     monkeypatch.setattr(abi, "rc_quant_workspace_bytes", lambda ctx, rows, batch: 1700 * rows)
     monkeypatch.setattr(RegionCacheModel, "__init__", lambda self: None)
     m = RegionCacheModel()
-    m.ctx, m.device, m.L, m._ws = None, "cpu", 2, {}
+    m.ctx, m.device, m.L, m._ws, m._quant = None, "cpu", 2, {}, None
     m._quantizable = [{f: torch.zeros(4, 4) for f in ("qkv_w", "fc1_w", "fc2_w")} for _ in range(2)]
     return m
 
@@ -27,3 +27,28 @@ def test_pools_have_workspaces_of_their_own(model):
     assert more.numel() == 40000 and model.workspace(10, 1, 8) is eight
     model.workspace(90, 1, 8)
     assert model.workspace(40, 1) is more
+
+
+def test_weights_stay_where_captured_steps_read_them(model, monkeypatch):
+    """Made once, made anew in place, and kept while the bf16 weights are in use."""
+    calls, given = [], []
+
+    class Matrix:
+        def struct(self):
+            return abi.rc_qmat(id(self))
+
+    def quantize(t, block_rows=1, out=None):
+        calls.append(out)
+        return out or Matrix()
+
+    def put(ctx, layers):
+        given.append(layers and [[getattr(layer, f).data for f, _ in abi.rc_quant_layer._fields_] for layer in layers])
+
+    monkeypatch.setattr(quant, "quantize", quantize)
+    monkeypatch.setattr(abi, "rc_set_quant_weights", put)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: None)
+    for enable in (True, True, False, True):
+        model.quantize_weights(enable)
+    assert given[0] == given[1] == given[3] and given[2] is None
+    assert len({p for layer in given[0] for p in layer}) == 6
+    assert calls[:6] == [None] * 6 and len(calls) == 18 and {id(c) for c in calls[6:]} == {p for layer in given[0] for p in layer}

@@ -27,6 +27,18 @@ LaunchTiming &launch_timing() {
   static thread_local LaunchTiming t;
   return t;
 }
+
+// Whole 128-byte lines of a matrix that a later kernel reads: the bfloat16
+// one of `lines` lines, or the 8-bit one that takes its place (up to its last
+// row's last value).
+struct WarmRange {
+  const void *p;
+  long long lines;
+};
+WarmRange warm_range(const void *w, long long lines, const rc_qmat *q) {
+  if (!q) return {w, lines};
+  return {q->data, ((q->rows - 1LL) * q->ld + q->cols) / 128};
+}
 }  // namespace rc
 
 namespace {
@@ -602,11 +614,15 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
   // MLP-up GEMM.  Where the cross query is a GEMM of its own its cross-attention
   // warms nothing: with the same lines warmed by that GEMM, steps of 1640 to
   // 16384 rows took 0.995 to 1.005 of the time, within a run's spread.
+  // With 8-bit weights the MLP's are those that the step reads (their products
+  // warm nothing).
   auto wlines = [&](long long n, long long k) { return n * k * (long long)c->esz / 128; };
-  const long long fc2_lines = wlines(C, F), fc2_half = fc2_lines / 2;
   bool a1_ready = false;  // the previous block's MLP reduction already wrote this block's LN1 rows
   for (int l = 0; l < L; ++l) {
     const rc_layer_weights &lw = c->layers[l];
+    const rc::WarmRange fc1_warm = rc::warm_range(lw.fc1_w, wlines(F, C), q_mm ? &c->quant[l].fc1_w : nullptr);
+    const rc::WarmRange fc2_warm = rc::warm_range(lw.fc2_w, wlines(C, F), q_mm ? &c->quant[l].fc2_w : nullptr);
+    const long long fc2_half = fc2_warm.lines / 2;
     char *qslot = quant ? cb + quant_slot_offset(c, T_, 0, step, l) : nullptr;
     T *slot = hp      ? (T *)(hp->staging + (size_t)(l % kRing) * hp->entry_bytes)
               : quant ? nullptr
@@ -697,8 +713,8 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
       a.O = O; a.total_rows = R; a.scale_log2 = scale_log2;
       a.q_x = A1; a.q_w = lw.xq_w; a.q_b = lw.xq_b;
       if (!xq_gemm) {
-        a.warm = dense ? lw.fc1_w : lw.fc2_w;
-        a.warm_lines = dense ? wlines(F, C) : fc2_half;
+        a.warm = dense ? fc1_warm.p : fc2_warm.p;
+        a.warm_lines = dense ? fc1_warm.lines : fc2_half;
       }
       if (emit) {
         a.n_delta = io->n_delta;
@@ -725,8 +741,8 @@ rc_status run_step(rc_ctx *c, const rc_cache_view *cache, int step, const rc_ste
         g.fold_shift[0] = lw.sst + 3 * C; g.fold_shift[1] = t0 + 3 * C;
         g.fold_stats = fstats; g.fold_nt = fold_nt; g.fold_extra = fextra;
       }
-      if (!dense) { g.warm = (const char *)lw.fc2_w + fc2_half * 128; g.warm_lines = fc2_lines - fc2_half; }
-      else { g.warm = lw.fc2_w; g.warm_lines = fc2_lines; }
+      g.warm = fc2_warm.p; g.warm_lines = fc2_warm.lines;
+      if (!dense) { g.warm = (const char *)g.warm + fc2_half * 128; g.warm_lines -= fc2_half; }
       RC_TRY(gemm<T>(c, RC_KC_GEMM_XPROJ, g, rc::EPI_RESID, gpart, gpf, s));
     }
     if (q_mm) {  // MLP from 8-bit weights, its inner activations in 8 bits; merge into the cached hidden state

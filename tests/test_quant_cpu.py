@@ -319,3 +319,19 @@ def test_attention_scale_limit(scale):
     rows = aset([0, 5, 9], idx=None)
     assert abi.LIB.rc_qcache_attention(C.byref(qcache()), C.byref(rows), None, FAKE, 288, scale, FAKE, 288, FAKE, 1 << 40,
                                        None) == -1
+
+
+class _Range(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("lines", C.c_longlong)]
+
+
+@pytest.mark.parametrize("rows,cols,ld", [(4608, 1152, 1152), (1152, 4608, 4608), (1152, 4608, 4624), (1, 16, 16), (3, 48, 4096)])
+def test_what_is_warmed_is_what_is_read(rows, cols, ld):
+    """A step's kernels warm the weights that its later products read: whole lines inside the 8-bit matrix where there
+    is one, else the bfloat16 one's."""
+    f = abi.LIB._ZN2rc10warm_rangeEPKvxPK7rc_qmat
+    f.restype, f.argtypes = _Range, [C.c_void_p, C.c_longlong, C.POINTER(abi.rc_qmat)]
+    r = f(2 * FAKE, 1000, C.byref(qmat(rows=rows, cols=cols, ld=ld, block_rows=128)))
+    assert r.p == FAKE and 0 <= ((rows - 1) * ld + cols) - r.lines * 128 < 128
+    r = f(2 * FAKE, 1000, None)
+    assert r.p == 2 * FAKE and r.lines == 1000

@@ -433,8 +433,9 @@ rc_status rc_qcache_store(const rc_qcache *cache, const rc_active_set *active, c
  * and every query row r of chain b, over keys j < key_len[b] of that chain.
  * rows: the chains' row ranges (offsets and offsets_host; idx is not read, and
  * the counts are not bounded by tokens).  key_len: device int32 [batch], clamped
- * to 0 .. tokens, or NULL for all tokens; rows of a chain without keys are 0.
- * What the cache holds behind key_len is not used, whatever it is.  q, out:
+ * to 0 .. tokens, or NULL for all tokens; rows of a chain without keys are 0,
+ * and rows of finite queries whose scores are all -infinity in float32.  What
+ * the cache holds behind key_len is not used, whatever it is.  q, out:
  * device bfloat16, heads side by side, rows ldq / ldo elements apart
  * (multiples of 8).  scratch: 16-byte aligned device memory of
  * rc_qcache_attention_scratch_bytes(cache, rows) bytes (may be NULL where that

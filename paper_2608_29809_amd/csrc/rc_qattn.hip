@@ -390,7 +390,7 @@ template <int QH> __global__ __launch_bounds__(256, 2) void qattn_kernel(QAttnAr
     const int q_base = q0 + wave * WQ + hh * 32, my_q = q_base + r32;
     auto put = [&](int q, int d, const f32x4 v, float den) {
       if (a.splits == 1) {
-        const float inv = 1.0f / den;
+        const float inv = den == 0.0f ? 0.0f : 1.0f / den;  // (0: every score is -infinity)
         *(bf16x4 *)(a.out + q * a.ldo + h * D + d) =
             bf16x4{(bf16)(v[0] * inv), (bf16)(v[1] * inv), (bf16)(v[2] * inv), (bf16)(v[3] * inv)};
       } else {
@@ -411,7 +411,7 @@ template <int QH> __global__ __launch_bounds__(256, 2) void qattn_kernel(QAttnAr
     }
     if (a.splits > 1 && g == 0 && my_q < r1) {
       float *ml = a.ml + (((size_t)split * a.total_rows + my_q) * heads + h) * 2;
-      ml[0] = m_ref[hh];
+      ml[0] = l_tot == 0.0f ? -INFINITY : m_ref[hh];  // (a range whose scores are all -infinity counts as one without keys)
       ml[1] = l_tot;
     }
   }

@@ -5,7 +5,7 @@ import torch
 
 import _quant_plans as P
 import _quant_ref as R
-from test_quant_gpu import Q, dev, matrix, product, rnd  # noqa: F401  (Q: a fixture)
+from test_quant_gpu import KERNELS, Q, check_attention, dev, matrix, product, random_cache, rnd, rows_set  # noqa: F401  (Q: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +31,32 @@ def test_product_of_two_steps_a_tile(Q, gelu):
         tol = 1.13 * tol + 2.0 ** -19 * ref.abs()
     tol += 2.0 ** -8 * ref.abs() + 1e-38
     assert ((y - ref).abs() <= tol).all()
+
+
+def put(cache, v, e):
+    """Values and scale bytes into the cache."""
+    cache.data.copy_(torch.from_numpy(v).float().to(torch.float8_e4m3fn))
+    cache.scales.copy_(torch.from_numpy(e).to(torch.uint8))
+
+
+@pytest.mark.parametrize("heads,tokens,rows", KERNELS)
+@pytest.mark.parametrize("share", [0.5, 1.0])
+def test_attention_scores_beyond_float32(Q, heads, tokens, rows, share):
+    """Finite queries and keys whose product is below the least float32, in whole key ranges: such keys have no weight
+    beside keys with logits near -720 (whose float32 error is below 2^-13, 2^-12 of mean |v| in the result), and where
+    there are no others the row is 0."""
+    nb = tokens // 64
+    far = np.arange(nb) < max(1, round(nb * share)) if nb > 1 else np.array([share == 1.0])
+    cache, v, e, *_ = random_cache(Q, 1, heads, nb, seed=rows)
+    v[:, :, far, 0], e[:, :, far, 0] = 0.0, 230
+    v[:, :, far, 0, :, 0] = -448.0      # times 2^103
+    v[:, :, ~far, 0, :, 0] = -192.0     # times 2^-35
+    e[:, :, ~far, 0] = 92
+    put(cache, v, e)
+    q = rnd(torch.bfloat16, rows, heads * 72, seed=1, std=3e8)
+    q[:, ::72] = 2.0 ** 40
+    o = Q.qcache_attention(cache, rows_set([rows]), dev(q, torch.bfloat16))
+    if share == 1.0:
+        assert (o == 0).all()
+    else:
+        check_attention(o, v, e, [rows], [tokens], q)

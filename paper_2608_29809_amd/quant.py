@@ -36,8 +36,10 @@ _SCALE = 1.0 / math.sqrt(HEAD_DIM)
 
 # The kernels of small calls take 3 to 7 us, a launch 3.2, so the host's time is a
 # call's time: torch.cuda.current_stream would add 2.8 us, current_device 0.2, sizes
-# as a tuple 0.35 to each torch.empty.
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+# as a tuple 0.35 to each torch.empty.  The quick lookups are private names of
+# PyTorch; where they are missing the public ones serve.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:

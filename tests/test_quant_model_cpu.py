@@ -52,3 +52,18 @@ def test_weights_stay_where_captured_steps_read_them(model, monkeypatch):
     assert given[0] == given[1] == given[3] and given[2] is None
     assert len({p for layer in given[0] for p in layer}) == 6
     assert calls[:6] == [None] * 6 and len(calls) == 18 and {id(c) for c in calls[6:]} == {p for layer in given[0] for p in layer}
+
+
+def test_without_private_names_of_torch(monkeypatch):
+    """The module's stream and device lookups fall back to PyTorch's public ones."""
+    import importlib.util
+    for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        monkeypatch.delattr(torch._C, name, raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda index: type("S", (), {"cuda_stream": 100 + index})())
+    spec = importlib.util.spec_from_file_location("paper_2608_29809_amd._quant_again", quant.__file__)
+    again = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(again)
+    got = []
+    again._call(lambda *args: got.append(args), 3, "x")
+    assert got == [("x", 103)]

@@ -6,6 +6,31 @@ import torch
 import _quant_aimed as A
 import _quant_plans as P
 from test_quant_aimed_gpu import CASES, LONG_FEW
+from test_quant_gpu import LARGE, SIZES
+from test_quant_tiles_gpu import PRODUCTS, STEPS
+
+SMALL = [(16, 16), (32, 32), (64, 32), (64, 64), (64, 128), (128, 128)]
+BIG = [(192, 256), (256, 256)]
+
+
+def test_products_of_the_tests_reach_every_tile():
+    """Every tile that has an epilogue, with every type of its results."""
+    seen = set()
+    for m, n, k in SIZES:
+        epi = "gelu" if m % 2 else "store"
+        seen |= {(P.product_tile(m, n, k, epi, n % 8 == 0), epi, "bf16"), (P.product_tile(m, n, k, epi, False), epi, "f32")}
+    for m, n, k, _ in LARGE:
+        seen |= {(P.product_tile(m, n, k, epi), epi, "bf16") for epi in ("store", "gelu")}
+    for m, n, k, gelu, f32 in PRODUCTS:
+        epi = "gelu" if gelu else "store"
+        seen.add((P.product_tile(m, n, k, epi, not f32), epi, "f32" if f32 else "bf16"))
+    rows = [chains * active for chains, active in STEPS] + [4096] + [29, 70, 93, 512, 8000, 10240]  # (the other steps')
+    for m in rows:
+        seen |= {(P.product_tile(m, 4608, 1152, "gelu8"), "gelu8", "e4m3"), (P.product_tile(m, 1152, 4608, "resid"), "resid", "f32")}
+    want = {(t, epi, out) for t in SMALL for epi in ("store", "gelu") for out in ("bf16", "f32")}
+    want |= {(t, epi, "bf16") for t in BIG for epi in ("store", "gelu")}
+    want |= {(t, "gelu8", "e4m3") for t in SMALL[4:] + BIG} | {(t, "resid", "f32") for t in SMALL[2:] + BIG}
+    assert seen == want
 
 
 def test_attention_cases_reach_every_kernel():

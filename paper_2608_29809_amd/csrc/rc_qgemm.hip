@@ -533,9 +533,12 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
   constexpr int FN = 8, BM = 32 * FM, BN = 32 * FN, W0 = BM * kQBlock, STAGE = W0 + BN * kQBlock;
   constexpr int NA = FM, NW = FN;  // copies of a stage: rows, W
   constexpr bool GELU = EPI == QG_GELU || EPI == QG_GELU8;
-  // per slot: rows, W; behind the ring, per slot: the rows' scales, W's four; for two tiles: the bias
+  // per slot: rows, W; behind the ring, per slot: the rows' scales, W's four; for
+  // three tiles: the bias (the next one's is copied before the last two steps of
+  // a tile, which are all of them if K = 256: another wave may still be in the
+  // epilogue of the tile before)
   constexpr int SCALES = 2 * STAGE, BIAS = SCALES + 2 * 512;
-  __shared__ __attribute__((aligned(1024))) char lds[BIAS + 2 * 4 * BN];
+  __shared__ __attribute__((aligned(1024))) char lds[BIAS + 3 * 4 * BN];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   __builtin_assume(wave >= 0 && wave < 4);
   const int wm = wave >> 1, wn = wave & 1, l16 = lane & 15, lq = lane >> 4;
@@ -614,7 +617,8 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
   int m0, n0;
   place(blockIdx.x, m0, n0);
   enter(m0, n0);
-  if (!g.bias) *(f32x2 *)(lds + BIAS + tid * 8) = f32x2{0.0f, 0.0f};
+  if (g.bias) copy_bias(n0, 0);
+  else if (tid < 3 * BN / 4) *(f32x4 *)(lds + BIAS + tid * 16) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     copy_scales(s);
@@ -668,10 +672,6 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
   for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
     int next_m0 = m0, next_n0 = n0;
     if (t + (int)gridDim.x < tiles) place(t + gridDim.x, next_m0, next_n0);
-    // (the last tile's epilogue, in which another wave may still be, reads the
-    // other place; the one before it is over, a step's barriers ago.  The copy is
-    // older than the first step's, whose wait and barrier make it everybody's)
-    if (g.bias) copy_bias(n0, which);
     const int byte = (n0 / kQBlock & 3) + wn, next_byte = (next_n0 / kQBlock & 3) + wn;
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -689,6 +689,7 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
       if (i < n) {
         if (t + (int)gridDim.x < tiles) {
           enter(next_m0, next_n0);
+          if (g.bias) copy_bias(next_n0, which == 2 ? 0 : which + 1);
         } else {  // no next one: the last stage again
           c_a -= by;
           c_w -= by;
@@ -706,7 +707,7 @@ __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int ti
     const char *bias_at = lds + BIAS + which * 4 * BN + (wn * 128 + lq * 4) * 4;
     m0 = next_m0;
     n0 = next_n0;
-    which ^= 1;
+    which = which == 2 ? 0 : which + 1;
     if constexpr (EPI == QG_RESID) {
       // half a row block of 16 at a time, its X and place loaded one half ahead
       // (rows and columns behind the last: any valid ones)

@@ -372,7 +372,9 @@ rc_status rc_compact_mask(const uint8_t *mask, int32_t batch, int32_t tokens, in
  * largest finite magnitude is at most 448 units, and round to nearest even;
  * values that are not finite become NaN and do not count for the scale.  (A
  * float32 of more than 1.9375 * 2^127 becomes 2^128, an infinity to the calls
- * that read it.)
+ * that read it; magnitudes below 2^-133, which only blocks with e <= 2 hold, are
+ * rounded to a multiple of it by products with float32 results and by the
+ * attention.)
  * These calls take no context.  They follow the conventions above: buffers
  * belong to the caller, work goes to `stream` of the current device, nothing
  * synchronises, nothing is kept between calls, and each may be captured into a
@@ -380,12 +382,13 @@ rc_status rc_compact_mask(const uint8_t *mask, int32_t batch, int32_t tokens, in
 
 /* A matrix [rows][cols] with a scale for each block_rows x 128 block:
  * block_rows 1 for activations, 128 for weights.  Blocks at the right and
- * lower edge are smaller where rows or cols end inside one. */
+ * lower edge are smaller where rows or cols end inside one.  At most 2^27 rows
+ * times column blocks (RC_ERR_SHAPE). */
 typedef struct {
   void *data;          /* device e4m3, rows `ld` bytes apart */
   uint8_t *scales;     /* device: entry (column block j, row block i) is scales[j*scale_ld + i];
                           read up to a multiple of 16 row blocks, whatever stands there */
-  int64_t ld;          /* a multiple of 16, >= cols */
+  int64_t ld;          /* a multiple of 16, cols to 2^20 */
   int32_t rows, cols;  /* cols a multiple of 16, at most 65536 */
   int32_t scale_ld;    /* a multiple of 16, >= row blocks */
   int32_t block_rows;  /* 1 or 128 */

@@ -14,9 +14,12 @@
 //   ring of six; fragments are read as 8-bit values (half of the LDS traffic
 //   that bounds the bfloat16 kernel at QH = 1) and converted in registers, once
 //   for QH 32x32 units.  (Tiles made bfloat16 in LDS once per workgroup take 18
-//   conversions per wave instead of 80, but three passes through LDS: 38.5
-//   against 36.8 us for 723 queries of 4096 keys, 1221 against 1216 for 16384
-//   of 16384.)
+//   conversions per wave instead of 80, but three passes through LDS: 5 % slower
+//   for 723 queries of 4096 keys, no faster for 16384 of 16384.)
+// * Of the ring only half a tile's time hides a copy: the register of scale
+//   bytes, loaded anew every 64 tiles, is read at the start of each, and the
+//   compiler's wait for it, in a loop whose copies it does not know of, is one
+//   for all of them.
 // * A partial last tile: keys and values behind the last become zeros in LDS,
 //   and dim 72 of those keys, which meets +-1 in the queries, is -3.4e38, so
 //   that no other place knows about masks.
@@ -25,7 +28,9 @@
 //   relative precision over the whole exponent range.  A workgroup one of whose
 //   denominators is not inside [2^-40, 2^80] (or is NaN), or one of whose sums
 //   of values is not finite, starts again relative to each query's maximum plus
-//   24 (probabilities of at most 2^-24).
+//   24 (probabilities of at most 2^-24).  Logits above 55 lead there, or a query
+//   whose logits are all below -28: where every workgroup does, 723 queries of
+//   4096 keys take 58 us instead of 33, 16384 of 16384 2860 instead of 1170.
 #include "rc_common.h"
 #include "rc_launch.h"
 #include "rc_quant.h"
@@ -51,7 +56,7 @@ __device__ __forceinline__ void lds_barrier8() { asm volatile("s_waitcnt lgkmcnt
 // XCDs, so that each has a part of every chain, however ragged the chains' rows
 // and keys are, and the query tiles that read the same keys are on one XCD.
 // Within an XCD the query tiles are outermost, so that a long chain's are on
-// different CUs.  (Six chains of 0..655 rows and 0..4096 keys 44 us; heads
+// different CUs.  (Six chains of 0..655 rows and 0..4096 keys in a graph 44 us; heads
 // outermost 54, a busy tile on every eighth CU; chains outermost 109.)
 // The grid holds the query tiles of all chains, or for more chains than the
 // arguments hold the longest one's for each.
@@ -420,11 +425,12 @@ template <int QH> __global__ __launch_bounds__(256, 2) void qattn_kernel(QAttnAr
 // Few queries (at most 16 of a chain per workgroup): bound by the cache's
 // bytes, so each of eight waves streams tiles of its own (every eighth of the
 // key range) through a ring of two without a barrier, with a running maximum,
-// and the waves' results are joined in LDS.  (Two workgroups of four waves on a
-// CU need twice the key splits: 64 queries of 4096 keys 14.0 instead of 13.3 us,
-// 33 of 16384 22.5 instead of 21.1.)  One query of 16384 keys: 15.6 us with its
-// combine, 38 MB or 7.4 us of the cache; 11 splits, in which a wave takes two or
-// three tiles, then the ends and the second launch.  16x16x32 blocks: rows m of two 16-key
+// and the waves' results are joined in LDS.  (The ring is drained at each tile:
+// the wait for the scale bytes, as above.  Two workgroups of four waves on a
+// CU need twice the key splits: 64 queries of 4096 keys and 33 of 16384 took 5
+// and 7 % longer.)  One query of 16384 keys: 14.5 us with its combine, 38 MB or
+// 7.4 us of the cache; 11 splits, in which a wave takes two or three tiles, then
+// the ends and the second launch.  16x16x32 blocks: rows m of two 16-key
 // operands are keys (m>>2)*8 + (m&3) and those + 4 of 32, so that a lane's
 // eight scores are those of the eight keys that PV takes from it.
 constexpr int kFewWaves = 8;
@@ -618,11 +624,13 @@ __global__ __launch_bounds__(64) void qattn_combine_kernel(QAttnArgs a) {
 // at about 4 TB/s.  Of the kernel for few queries a wave takes a tile in 1.75 us,
 // a workgroup's ends take 3, one after the other on a CU (33 queries of 16384 keys
 // in 5, 10 and 16 splits 21.1, 24.8 and 27.6), and the cache's bytes at most 5.5
-// TB/s.  Best of each with its combine, us (few, QH = 1, QH = 2): one query of
-// 16384 keys 15.6, 26.5; one of 4096 10.1, 13.7; 64 of 4096 13.3, 16.2; 154 of 4096
-// 20.7, 24.5; 154 of 16384 QH = 1 39; 723 of 4096 36.8 (five splits) and 38.9; 1639 of
-// 4096 63.4 and 59.7; 4096 of 4096 98.2 and 101.9; 1639 of 16384 182 and 162; 16384 of
-// 16384 1398 and 1175.
+// TB/s.  Best of each with its combine, us in a captured graph (on a stream, where
+// a launch overlaps the end of the one before, 2 to 4 less; few, QH = 1, QH = 2):
+// one query of 16384 keys 16.4, 26.6, 34.2; one of 4096 10.8, 13.9, 16.1; 64 of
+// 4096 13.9, 16.6, 19.2; 154 of 4096 19.4, 23.0, 24.8; 154 of 16384 51, 37.1, 39.4;
+// 723 of 4096 QH = 1 37.2 (five splits), QH = 2 38.9; 1639 of 4096 61.4 and 59.1; 4096
+// of 4096 95.5 and 100.1; 1639 of 16384 170 and 159; 16384 of 16384 1396 and 1168.
+// (The constants hold the drain of the rings.)
 QAttnPlan plan_qattention(const int *offsets, int chains, int heads, int tokens) {
   const int n_tiles = tokens / kQTokens;
   const long long rows = offsets ? offsets[chains] : (long long)chains * tokens;

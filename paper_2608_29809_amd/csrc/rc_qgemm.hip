@@ -8,7 +8,7 @@
 // its 128 products is held to about 17 bits (measured: 1.3e-5 of the result's
 // norm, against 2.0e-3 for rounding it to bfloat16).
 // float32 results: the operands become bfloat16 with their scales applied
-// (exactly), for 16x16x32 instructions whose sums keep float32's precision
+// (exactly from 2^-133 on), for 16x16x32 instructions whose sums keep float32's precision
 // (8e-8 of the result's norm over 36 blocks, as a float32 library product).
 //
 // W is operand A of the matrix instruction, so a lane's accumulators are four
@@ -175,11 +175,13 @@ __global__ __launch_bounds__(64 * KG) void qgemm_split_kernel(QGemmArgs g) {
 // * KG > 1, one wave per group, for few tiles: nothing but its own copies is
 //   waited for, a block's fragments are read while the block before is
 //   multiplied, in the registers that its fragments leave, and the groups' sums
-//   are joined in LDS in a fixed order.
+//   are joined in LDS in a fixed order.  A step waits for the next block before
+//   it sends for the one after that, so S - 1 blocks are on their way at most.
 // What bounds it: with 128 x 128 tiles (4096 x 4608 x 1152 with GELU: 38 us, 1.1
 // PFLOP/s) LDS, which gives 128 bytes per clock and takes 187 for 64 x 64 wave
-// tiles with their copies, then the epilogues; with KG = 4 the copies' latency
-// (723 x 1152 x 4608, 64 x 64 tiles: 16 us, 34 with 128 x 128).
+// tiles with their copies, then the epilogues; with KG = 4 the copies' latency,
+// a whole one each step at S = 2 (723 x 1152 x 4608, 64 x 64 tiles: nine steps in
+// 14.5 us).
 template <int FM, int FN, int WGM, int WGN, int KG, int S, int EPI, typename OUT>
 __global__ __launch_bounds__(64 * WGM * WGN * KG, 2) void qgemm_kernel(QGemmArgs g) {
   constexpr int NG = WGM * WGN, NW = NG * KG, BM = 16 * FM * WGM, BN = 16 * FN * WGN;
@@ -521,13 +523,18 @@ template <int PLACE> __device__ __forceinline__ void lds_copy16(const void *from
 // * Copies are issued one between two products, every second or third (all at
 //   once they hold a wave up for 1100 clocks a step; with a branch each, 400).
 // * The steps of a workgroup's tiles are one sequence: the last two steps of a
-//   tile copy the next one's first stages, which arrive during the epilogue.
-//   That needs no LDS: lanes exchange registers until they hold whole stores.
+//   tile copy the next one's first stages, which are on their way when the
+//   epilogue begins.  It needs no LDS: lanes exchange registers until they hold
+//   whole stores.  (It does not overlap them: 4 to 15 registers are spilled,
+//   some are read back where the epilogue begins, and the wait for those is one
+//   for every copy too.  Spills are no danger to the counted waits: vector memory
+//   operations end in order, so one more between a copy and its wait can only
+//   make the wait longer.)
 // 2330 clocks a step where few CUs work; with all of them the power limit leaves
 // 1.8 GHz.  A tile's epilogue takes 6500 clocks, 17500 with GELU, of nine steps'
 // 21000 at K = 1152, and nothing covers it (accumulators of a second tile find
-// no registers).  16384 x 4608 x 1152: 99 us (128 x 128 tiles 118), 104 with GELU
-// (134); 8192 x 8192 x 9216: 462 us, 2.7 PFLOP/s.
+// no registers).  16384 x 4608 x 1152: 98 to 100 us (128 x 128 tiles 118), 102 to
+// 111 with GELU (134), by card; 8192 x 8192 x 9216: 462 us, 2.7 PFLOP/s.
 template <int FM, int EPI>
 __global__ __launch_bounds__(256, 1) void qgemm_large_kernel(QGemmArgs g, int tiles) {
   constexpr int FN = 8, BM = 32 * FM, BN = 32 * FN, W0 = BM * kQBlock, STAGE = W0 + BN * kQBlock;

@@ -4,9 +4,10 @@
 // Values are e4m3.  A block's scale is a power of two held as one byte e,
 // 2^(e - 127): the least with which its largest finite magnitude is at most
 // 448, and e >= 1.  A floating-point format loses no precision to a power of
-// two (only range), dequantised values are exact in bfloat16, a block's other
-// values are exact under a change of its scale (unless they become
-// subnormal), and the matrix instructions take the byte as it is.
+// two (only range), dequantised values are exact in bfloat16 (but for e <= 2,
+// where those below 2^-133 are beneath its range), a block's other values are
+// exact under a change of its scale (unless they become subnormal), and the
+// matrix instructions take the byte as it is.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -164,7 +165,7 @@ __device__ __forceinline__ float row16_max(float v) {
 typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-// Eight e4m3 values times a power of two, in bfloat16 (exact).
+// Eight e4m3 values times a power of two, in bfloat16 (exact from 2^-133 on).
 __device__ __forceinline__ bf16x8 q_bf16x8(u32x2 v, float factor) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[0], factor, false);
   const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[0], factor, true);

@@ -148,9 +148,9 @@ hipError_t launch_norm_quantize(const NormQuantArgs &a, hipStream_t s) {
 // first active row is among its `chunk` rows of the list.  A block's fresh rows
 // take the places of their tokens, the others keep their values; the scale is
 // that of the merged tile.  Bound by latency for a region (the list, then the
-// values and the old tile: 723 tokens of a 4096-token cache 6.9 us), by its bytes
-// for every token of a dense step (idx null: workgroup x takes block x): 16384
-// tokens from float32 73 us, 5.2 TB/s.
+// values and the old tile: 729 tokens of a 4096-token cache 6.8 us), by its bytes
+// for every token of a dense step (idx null: workgroup x takes block x): two
+// chains of 16384 tokens from float32 73 us, 5.2 TB/s.
 template <typename T> __global__ __launch_bounds__(192) void qcache_store_kernel(QStoreArgs a, int chunk) {
   constexpr int CPR = kHeadDim / 8;  // chunks of eight values per token
   __shared__ int row_of[kQTokens];

@@ -7,10 +7,15 @@ from test_quant_gpu import KERNELS, Q, rows_set  # noqa: F401  (Q: a fixture)
 
 pytestmark = pytest.mark.gpu
 
-# heads, tokens, query rows of the chains, key lengths: every kernel and split; several chains; more than 64 tiles (one
-# register of scale bytes) in a range of the kernels for one and for two query halves per wave
+# heads, tokens, query rows of the chains, key lengths: every kernel and split; several chains, and more than travel in
+# the arguments (heads x splits a multiple of eight, and not); more than 64 tiles (one register of scale bytes) in a range
+# of the kernels for one and for two query halves per wave
+MANY = tuple(1024 - 13 * b for b in range(20))
 CASES = [(h, t, (r,), (t - 27,)) for h, t, r in KERNELS] + [
     (2, 4096, (70, 0, 300, 5), (4096, 4096, 2500, 65)),
+    (2, 1024, (300,) * 12 + (0, 700) + (130,) * 6, MANY),
+    (16, 1024, (300,) * 20, MANY),
+    (16, 1024, (900,) * 20, MANY),
     (16, 5120, (10000,), (5101,)),
     (4, 16384, (16384,), (16380,)),
 ]

@@ -16,6 +16,8 @@ PRODUCTS = [
     (301, 2304, 400, False, True), (301, 2304, 400, True, True),      # 64 x 128, whole vectors of float32
     (301, 2304, 400, False, False),
     (1501, 4608, 272, False, True), (1501, 4608, 272, True, True),    # 128 x 128 likewise
+    (3, 40, 65536, False, False), (70, 200, 65536, True, True),       # the longest sum
+    (1501, 1160, 65536, False, False),
 ]
 # chains alike, active tokens of each: 128 x 128 tiles for the GELU results (1000, 1405 and 3650 rows), 64 x 128 and
 # 128 x 128 for the residual (1405 and 2000; 3650 and 4000); chains and the last tile end inside a tile

@@ -120,7 +120,7 @@ template <int L, int U, typename H> constexpr int kNormResident = L == 16 ? (kUp
 // without `chunk` loads the vectors for each (16384 x 1152: 30 us instead of 24.5); two
 // rows at a time, whose exchanges are one, were slower (26).
 template <int L, int U, int FORM, typename X, typename H>
-__global__ __launch_bounds__(L ? 256 : 1024, kNormResident<L, U, H>) void norm_kernel(NormArgs a, int chunk) {
+__global__ __launch_bounds__(L ? 256 : 1024, (kNormResident<L, U, H>)) void norm_kernel(NormArgs a, int chunk) {
   constexpr bool RES = kUpdate<H>;
   constexpr int G = L ? 256 / L : 1, LANES = L == 16 ? 16 : 64;  // rows of a workgroup at a time; lanes of a wave that share a row
   __shared__ float2 parts[L ? 1 : 2][2][kNormWaves];             // of post, pre; rows of even and odd number

@@ -165,6 +165,11 @@ typedef struct rc_ctx rc_ctx;
 /* Message of the last failed call on this thread ("" if none). */
 const char *rc_last_error(void);
 
+/* SHA-256 (64 hexadecimal digits) of the sources, headers and flags that this
+ * library was compiled from, as paper_2608_29809_amd/build.py's digest() gives it
+ * of the tree; "unknown" where another build compiled it. */
+const char *rc_source_digest(void);
+
 /* Validate the config, copy it and the weight pointers into a host-side
  * context.  Touches no device.  RC_ERR_UNSUPPORTED for shapes outside the
  * list above.  A context holds host-side state (timing records and, once a

@@ -3,13 +3,16 @@
 Argument marshalling only: every function here forwards to the C function of
 the same name and raises RcError on a negative status.  Nothing is computed
 in Python.  The library must have been built (paper_2608_29809_amd/build.py);
-importing this module without it raises immediately.
+importing this module without it, or with one that was built from other sources
+than those beside it, raises immediately.
 """
 from __future__ import annotations
 
 import ctypes as C
 import os
 import struct
+
+from . import build
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libregioncache.so")
@@ -126,12 +129,20 @@ def _load():
         raise ImportError(f"{LIB_PATH} is missing: build it with paper_2608_29809_amd/build.py "
                           "(or __graft_entry__.build())")
     lib = C.CDLL(LIB_PATH)
+    if os.path.isdir(build.CSRC):  # (beside its sources: structures that do not match them would be read as pointers)
+        of = getattr(lib, "rc_source_digest", None)
+        if of is not None:
+            of.restype, of.argtypes = C.c_char_p, []
+        if of is None or of().decode() != build.digest():
+            raise ImportError(f"{LIB_PATH} was built from other sources than those beside it: build it again with "
+                              "paper_2608_29809_amd/build.py (or __graft_entry__.build())")
     P, S, I32, U32 = C.c_void_p, C.c_size_t, C.c_int32, C.c_uint32
     pI32 = C.POINTER(C.c_int32)
     I64, QM, QC, AS = C.c_int64, C.POINTER(rc_qmat), C.POINTER(rc_qcache), C.POINTER(rc_active_set)
     IM = C.POINTER(rc_imat)
     sig = {
         "rc_last_error": (C.c_char_p, []),
+        "rc_source_digest": (C.c_char_p, []),
         "rc_create": (C.c_int, [C.POINTER(rc_model_config), C.POINTER(rc_weights), C.POINTER(P)]),
         "rc_destroy": (None, [P]),
         "rc_cache_bytes": (S, [P, I32, I32]),

@@ -1089,6 +1089,13 @@ extern "C" {
 
 const char *rc_last_error(void) { return g_err.c_str(); }
 
+#ifndef RC_SOURCE_DIGEST
+#define RC_SOURCE_DIGEST unknown  // (compiled by hand)
+#endif
+#define RC_TEXT_OF(x) #x
+#define RC_TEXT(x) RC_TEXT_OF(x)
+const char *rc_source_digest(void) { return RC_TEXT(RC_SOURCE_DIGEST); }
+
 rc_status rc_create(const rc_model_config *cfg, const rc_weights *w, rc_ctx **out) {
   g_err.clear();
   RC_CHECK(cfg && w && out, RC_ERR_INVALID_ARG, "null argument to rc_create");

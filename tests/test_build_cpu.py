@@ -5,7 +5,7 @@ import subprocess
 
 import pytest
 
-from paper_2608_29809_amd import build
+from paper_2608_29809_amd import abi, build
 
 SOURCES = sorted(f for f in os.listdir(build.CSRC) if f.endswith(".hip"))
 
@@ -32,3 +32,55 @@ def test_sources_compile():
     with concurrent.futures.ThreadPoolExecutor(max_workers=4) as ex:
         failed = {n: e for n, e in zip(SOURCES, ex.map(errors, SOURCES)) if e}
     assert not failed, failed
+
+
+def test_library_is_of_these_sources():
+    assert abi.LIB.rc_source_digest().decode() == build.digest()
+
+
+def test_library_of_other_sources_is_refused(monkeypatch):
+    monkeypatch.setattr(build, "digest", lambda: "0" * 64)
+    with pytest.raises(ImportError, match="other sources"):
+        abi._load()
+
+
+def test_digest_sees_every_source(monkeypatch, tmp_path):
+    """One byte more, another name or another flag is another digest; other files do not count."""
+    monkeypatch.setattr(build, "CSRC", str(tmp_path / "csrc"))
+    monkeypatch.setattr(build, "HEADER", str(tmp_path / "api.h"))
+    (tmp_path / "csrc").mkdir()
+    a, b, api = tmp_path / "csrc" / "a.hip", tmp_path / "csrc" / "b.h", tmp_path / "api.h"
+    for f in (a, b, api):
+        f.write_text("int x;\n")
+    seen = [build.digest()]
+    (tmp_path / "csrc" / "notes.txt").write_text("x")
+    assert build.digest() == seen[0]
+    for f in (a, b, api):
+        f.write_text("int x; \n")
+        seen.append(build.digest())
+    b.rename(tmp_path / "csrc" / "c.h")
+    seen.append(build.digest())
+    monkeypatch.setattr(build, "FLAGS", build.FLAGS + ["-g"])
+    seen.append(build.digest())
+    assert len(set(seen)) == len(seen)
+
+
+@pytest.mark.parametrize("fails", ["compile", "link", "edit"])
+def test_failed_build_leaves_no_library(monkeypatch, tmp_path, fails):
+    """The library of an earlier build does not stand for sources that were not built."""
+    for name in ("BUILD", "LIB", "CSRC", "HEADER"):
+        monkeypatch.setattr(build, name, str(tmp_path / name.lower()))
+    os.mkdir(build.CSRC)
+    source = tmp_path / "csrc" / "a.hip"
+    source.write_text("int x;\n")
+    (tmp_path / "header").write_text("")
+    (tmp_path / "lib").write_text("an earlier library")
+    compiler = tmp_path / "compiler"
+    compiler.write_text({"compile": "#!/bin/sh\nexit 1\n",
+                         "link": '#!/bin/sh\ntest "$1" != -shared\n',
+                         "edit": f'#!/bin/sh\nif test "$1" = -shared; then echo "int y;" > {source}; echo > {build.LIB}.tmp; fi\n'}[fails])
+    compiler.chmod(0o755)
+    monkeypatch.setattr(build, "hipcc", lambda: str(compiler))
+    with pytest.raises(RuntimeError):
+        build.build()
+    assert not os.path.exists(build.LIB)

@@ -33,40 +33,57 @@ Result = Union[torch.Tensor, QuantMatrix, IntMatrix]
 class Norm:
     """LayerNorm ("layer") or RMS norm ("rms") of rows, with weight and bias
     (float32 [cols]) or without.  Both are held as they lie in memory now:
-    changes in place are seen, another tensor put in a parameter's place is not."""
+    changes in place are seen, another tensor put in their place is not, and
+    where that memory is resized the norm is refused."""
 
-    __slots__ = ("_kind", "_eps", "_weight", "_bias", "_cols", "_struct", "_address")
+    __slots__ = ("_kind", "_eps", "_cols", "_index", "_weight", "_bias", "_struct", "_address")
 
     def __init__(self, kind: str = "layer", eps: float = 1e-6, weight: Optional[torch.Tensor] = None,
                  bias: Optional[torch.Tensor] = None):
         code = _KINDS.get(kind)
         if code is None:
             raise ValueError(f"norm {kind!r} is not 'layer' or 'rms'")
-        cols = at_weight = at_bias = None
+        cols = index = at_weight = at_bias = held_weight = held_bias = None
         if weight is not None:
-            weight, cols, at_weight = self._vector(weight, "weight")
+            cols, index, at_weight, held_weight = self._hold(weight, "weight")
         if bias is not None:
-            bias, cols_bias, at_bias = self._vector(bias, "bias")
+            cols_bias, index_bias, at_bias, held_bias = self._hold(bias, "bias")
             if weight is not None and cols != cols_bias:
                 raise ValueError(f"weight and bias have {cols} and {cols_bias} values")
-            cols = cols_bias
-        self._kind, self._eps, self._weight, self._bias, self._cols = kind, eps, weight, bias, cols
+            if weight is not None and index != index_bias:
+                raise ValueError(f"weight and bias are on {weight.device} and {bias.device}")
+            cols, index = cols_bias, index_bias
+        self._kind, self._eps, self._cols, self._index, self._weight, self._bias = kind, eps, cols, index, held_weight, held_bias
         self._struct = abi.rc_norm(code, eps, at_weight, at_bias)
         self._address = C.addressof(self._struct)
 
     @staticmethod
-    def _vector(t: torch.Tensor, what: str):
+    def _hold(t: torch.Tensor, what: str):
+        """Its width, device, address, and memory: a storage, where that lies and its bytes (a tensor may be given other memory)."""
         if t.dtype != _F32 or t.dim() != 1 or not t.is_contiguous():
             raise ValueError(f"{what} must be contiguous float32 [cols]")
-        if type(t) is not torch.Tensor:  # (a parameter's memory may be exchanged under its name)
-            t = t.detach()
-        return t, t.shape[0], t.data_ptr()
+        memory = t.untyped_storage()
+        return t.shape[0], t.get_device(), t.data_ptr(), (memory, memory.data_ptr(), memory.nbytes())
+
+    def _tensor(self, held, address) -> Optional[torch.Tensor]:
+        if held is None:
+            return None
+        _intact(held, "a norm's weights")
+        memory, start, _ = held
+        return torch.empty(0, dtype=_F32, device=memory.device).set_(memory, ((address or 0) - start) // 4, (self._cols,))
 
     # (read-only: the C structure is made once)
     kind = property(lambda self: self._kind)
     eps = property(lambda self: self._eps)
-    weight = property(lambda self: self._weight)
-    bias = property(lambda self: self._bias)
+    weight = property(lambda self: self._tensor(self._weight, self._struct.weight))
+    bias = property(lambda self: self._tensor(self._bias, self._struct.bias))
+
+
+def _intact(held, what: str) -> None:
+    """Refuses memory that was moved, freed or cut since it was held."""
+    memory, start, size = held
+    if memory.data_ptr() != start or memory.nbytes() != size:
+        raise ValueError(f"the memory of {what} was resized")
 
 
 def _vector(t: torch.Tensor, cols: int, rows: Optional[ActiveSet], index: int, what: str):
@@ -89,9 +106,12 @@ def _norm(norm: Norm, cols: int, index: int, what: str) -> int:
     if norm._cols is not None:
         if norm._cols != cols:
             raise ValueError(f"{what} has weights of {norm._cols} values, x {cols}")
-        for t in (norm._weight, norm._bias):
-            if t is not None and t.get_device() != index:
-                raise ValueError(f"the weights of {what} are on {t.device}, x on cuda:{index}")
+        if norm._index != index:
+            raise ValueError(f"the weights of {what} are on {'the CPU' if norm._index < 0 else f'cuda:{norm._index}'}, x on cuda:{index}")
+        if norm._weight is not None:
+            _intact(norm._weight, f"the weight of {what}")
+        if norm._bias is not None:
+            _intact(norm._bias, f"the bias of {what}")
     return norm._address
 
 

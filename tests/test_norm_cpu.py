@@ -131,3 +131,50 @@ def test_plain_form_in_float32():
             y = d / np.sqrt((d * d).mean(1, keepdims=True, dtype=np.float32) + np.float32(1e-6))
             ref, tol = R.norm(x.astype(np.float64), np.zeros(x.shape), kind, 1e-6)
             assert (np.abs(y - ref) <= tol).all(), (cols, off, kind)
+
+
+GIVEN = {"tensor": lambda t: t, "parameter": torch.nn.Parameter, "view": lambda t: torch.cat([t, t])[t.numel():]}
+
+
+@pytest.mark.parametrize("part", ["weight", "bias"])
+@pytest.mark.parametrize("given", GIVEN)
+def test_memory_of_weights(given, part):
+    """A norm holds the memory that it was made of; where that is resized it is refused instead of read."""
+    def made(**more):
+        t = GIVEN[given](torch.full((1152,), 2.0))
+        return t, norm.Norm("rms", **{part: t, **more})
+
+    def held(n):  # (as the C structure has it)
+        assert norm._norm(n, 1152, -1, "the norm") == C.addressof(n._struct)
+        assert getattr(n, part).data_ptr() == getattr(n._struct, part) and not getattr(n, part).requires_grad
+        return getattr(n, part)
+
+    t, n = made()
+    with torch.no_grad():
+        t.fill_(3.0)
+    assert held(n).data_ptr() == t.data_ptr() and torch.equal(held(n), torch.full((1152,), 3.0))
+    t.data = torch.zeros(4)
+    others = [torch.full((1152,), 5.0) for _ in range(64)]  # (the memory would be theirs)
+    assert torch.equal(held(n), torch.full((1152,), 3.0)) and len(others) == 64
+    t, n = made()
+    with torch.no_grad():
+        t.set_(torch.zeros(4))
+    assert torch.equal(held(n), torch.full((1152,), 2.0))
+    t, n = made()
+    getattr(n, part).set_(torch.zeros(4))  # (a tensor of that memory, not what the norm holds)
+    assert torch.equal(held(n), torch.full((1152,), 2.0))
+    for resize in (lambda t: t.detach().resize_(1 << 20), lambda t: t.untyped_storage().resize_(0), lambda t: t.untyped_storage().resize_(64)):
+        for more in ({}, {"weight" if part == "bias" else "bias": torch.zeros(1152)}):
+            t, n = made(**more)
+            resize(t)
+            with pytest.raises(ValueError, match="resized"):
+                norm._norm(n, 1152, -1, "the norm")
+            with pytest.raises(ValueError, match="resized"):
+                getattr(n, part)
+
+
+def test_weights_elsewhere():
+    n = norm.Norm(weight=torch.zeros(8))
+    assert norm._norm(n, 8, -1, "post")
+    with pytest.raises(ValueError, match="the CPU"):
+        norm._norm(n, 8, 0, "post")

@@ -145,18 +145,18 @@ def _run(x, h, gate, post, residual_scale, pre, scale, shift, rows, dtype, out):
                 pout = out.data_ptr()
             elif dtype == _I8:
                 out = IntMatrix._new(n, cols, index)
-                int8 = C.addressof(out._struct)
+                int8 = C.addressof(out.struct())
             elif dtype == _F8:
                 out = QuantMatrix.alloc(n, cols, 1, x.device)
-                e4m3 = C.addressof(out._struct)
+                e4m3 = C.addressof(out.struct())
             else:
                 raise ValueError(f"dtype {dtype} is not float32, bfloat16, float8_e4m3fn or int8")
         elif isinstance(out, IntMatrix):
             _on_gpu(x, out._data)
-            int8 = C.addressof(out._struct)
+            int8 = C.addressof(out.struct())
         elif isinstance(out, QuantMatrix):
             _on_gpu(x, out._data)
-            e4m3 = C.addressof(out._struct)
+            e4m3 = C.addressof(out.struct())
         else:
             _on_gpu(x, out)
             pout, ldo, out_dtype = out.data_ptr(), _ld(out, n, cols, "out"), _dtype(out, "out")

@@ -95,12 +95,45 @@ def _ld(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
     return ld if rows > 1 else max(cols, ld)
 
 
-class QuantMatrix:
+class _InMemory:
+    """Tensors `data` and `scales` with a C structure of their addresses and
+    sizes, made once: where the tensors were given other memory since (set_,
+    resize_, .data) it is refused."""
+
+    __slots__ = ("_data", "_scales", "_struct", "_memory")  # (_memory: None while nobody else has seen the tensors)
+
+    def _seen(self) -> None:
+        data, scales = self._data, self._scales
+        of_data, of_scales = data.untyped_storage(), scales.untyped_storage()  # (kept: what the structure points to is not freed)
+        self._memory = data.data_ptr(), of_data, of_data.nbytes(), scales.data_ptr(), of_scales, of_scales.nbytes()
+
+    @property
+    def data(self) -> torch.Tensor:
+        if self._memory is None:
+            self._seen()
+        return self._data
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._memory is None:
+            self._seen()
+        return self._scales
+
+    def struct(self):
+        if self._memory is not None:
+            data, of_data, data_bytes, scales, of_scales, scales_bytes = self._memory
+            if (self._data.data_ptr() != data or of_data.nbytes() != data_bytes or self._scales.data_ptr() != scales
+                    or of_scales.nbytes() != scales_bytes):
+                raise ValueError(f"the memory of a {type(self).__name__}'s tensors was exchanged or resized")
+        return self._struct
+
+
+class QuantMatrix(_InMemory):
     """A matrix in 8 bits: `data` float8_e4m3fn [rows, cols], `scales` uint8
     [column blocks, row blocks rounded up to 16], block_rows 1 or 128.  Views
     of rows are given as data[:n] with the same scales."""
 
-    __slots__ = ("_data", "_scales", "_block_rows", "_struct")
+    __slots__ = ("_block_rows",)
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor, block_rows: int):
         if data.dtype != _F8 or data.dim() != 2:
@@ -115,12 +148,10 @@ class QuantMatrix:
         _on_gpu(data, scales)
         ld = cols if data.is_contiguous() else _ld(data, rows, cols, "data")
         self._data, self._scales, self._block_rows = data, scales, block_rows
+        self._seen()
         self._struct = abi.rc_qmat(data.data_ptr(), scales.data_ptr(), ld, rows, cols,
                                    row_blocks if col_blocks == 1 else scales.stride(0), block_rows)
 
-    # (read-only: the C structure is made once)
-    data = property(lambda self: self._data)
-    scales = property(lambda self: self._scales)
     block_rows = property(lambda self: self._block_rows)
 
     @classmethod
@@ -134,19 +165,16 @@ class QuantMatrix:
         row_blocks += -row_blocks % 16
         m._data = data = torch.empty(rows, cols, dtype=_F8, device=device)
         m._scales = scales = torch.empty(-(-cols // BLOCK), row_blocks, dtype=_U8, device=device)
-        m._block_rows = block_rows
+        m._block_rows, m._memory = block_rows, None
         m._struct = abi.rc_qmat(data.data_ptr(), scales.data_ptr(), cols, rows, cols, row_blocks, block_rows)
         return m
 
-    def struct(self) -> abi.rc_qmat:
-        return self._struct
 
-
-class IntMatrix:
+class IntMatrix(_InMemory):
     """A matrix in int8 with a scale for each row: `data` int8 [rows, cols],
     `scales` float32 [rows].  Views of rows are given as data[:n], scales[:n]."""
 
-    __slots__ = ("_data", "_scales", "_struct")
+    __slots__ = ()
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor):
         shape = data.shape
@@ -159,12 +187,9 @@ class IntMatrix:
             raise ValueError(f"{rows} x {cols} is too large")
         _on_gpu(data, scales)
         self._data, self._scales = data, scales
+        self._seen()
         ld = cols if data.is_contiguous() else _ld(data, rows, cols, "data")
         self._struct = abi.rc_imat(data.data_ptr(), scales.data_ptr(), ld, rows, cols)
-
-    # (read-only: the C structure is made once)
-    data = property(lambda self: self._data)
-    scales = property(lambda self: self._scales)
 
     @classmethod
     def alloc(cls, rows: int, cols: int, device="cuda") -> "IntMatrix":
@@ -181,21 +206,18 @@ class IntMatrix:
     @classmethod
     def _of(cls, data: torch.Tensor, scales: torch.Tensor, rows: int, cols: int) -> "IntMatrix":
         m = cls.__new__(cls)
-        m._data, m._scales = data, scales
+        m._data, m._scales, m._memory = data, scales, None
         m._struct = abi.rc_imat(data.data_ptr(), scales.data_ptr(), cols, rows, cols)
         return m
 
-    def struct(self) -> abi.rc_imat:
-        return self._struct
 
-
-class QuantCache:
+class QuantCache(_InMemory):
     """Keys and values of `batch` chains in 8 bits: `data` float8_e4m3fn
     [batch, heads, blocks, 2, 64, 72] (a block's 64 keys, then its values) and
     `scales` uint8 [batch, heads, blocks, 2].  Chains may be any multiple of
     16 bytes apart; within a chain the cache is contiguous."""
 
-    __slots__ = ("_data", "_scales", "_struct", "batch", "heads", "tokens")
+    __slots__ = ("batch", "heads", "tokens")
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor):
         if data.dtype != _F8 or data.dim() != 6:
@@ -211,13 +233,10 @@ class QuantCache:
             raise ValueError("a chain of the cache must be contiguous")
         _on_gpu(data, scales)
         self._data, self._scales = data, scales
+        self._seen()
         self.batch, self.heads, self.tokens = batch, heads, blocks * KEY_BLOCK
         self._struct = abi.rc_qcache(data.data_ptr(), scales.data_ptr(), data.stride(0), scales.stride(0), batch, heads,
                                      self.tokens)
-
-    # (read-only: the C structure is made once)
-    data = property(lambda self: self._data)
-    scales = property(lambda self: self._scales)
 
     @classmethod
     def alloc(cls, batch: int, heads: int, tokens: int, device="cuda") -> "QuantCache":
@@ -227,9 +246,6 @@ class QuantCache:
         shape = (batch, heads, tokens // KEY_BLOCK, 2)
         return cls(torch.zeros(shape + (KEY_BLOCK, HEAD_DIM), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn),
                    torch.zeros(shape, dtype=torch.uint8, device=device))
-
-    def struct(self) -> abi.rc_qcache:
-        return self._struct
 
 
 def quantize(x: torch.Tensor, block_rows: int = 1, out: Optional[QuantMatrix] = None) -> QuantMatrix:
@@ -245,11 +261,11 @@ def quantize(x: torch.Tensor, block_rows: int = 1, out: Optional[QuantMatrix] = 
         index = _on_gpu(x)
         out = QuantMatrix.alloc(rows, cols, block_rows, x.device)
     else:
-        index = _on_gpu(x, out.data)
-        if out.data.shape != x.shape or out.block_rows != block_rows:
+        index = _on_gpu(x, out._data)
+        if (out._struct.rows, out._struct.cols) != x.shape or out.block_rows != block_rows:
             raise ValueError("out has another shape or other blocks")
     if rows:
-        _call(abi.rc_quantize, index, x.data_ptr(), dtype, ldx, C.byref(out._struct))
+        _call(abi.rc_quantize, index, x.data_ptr(), dtype, ldx, C.byref(out.struct()))
     return out
 
 
@@ -257,17 +273,17 @@ def qgemm(a: QuantMatrix, w: QuantMatrix, bias: Optional[torch.Tensor] = None, g
           dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """act(a w^T + bias): a [m, k] with block_rows 1, w [n, k] with block_rows
     128, bias float32 [n]; the result [m, n] in dtype (or in out)."""
-    A, W = a._struct, w._struct
+    A, W = a.struct(), w.struct()
     m, n = A.rows, W.rows
     if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,) or not bias.is_contiguous()):
         raise ValueError(f"bias must be contiguous float32 [{n}]")
     if out is None:
         if dtype not in _DTYPES:
             raise ValueError(f"dtype {dtype} is not float32 or bfloat16")
-        out, ldo = torch.empty(m, n, dtype=dtype, device=a.data.device), n
+        out, ldo = torch.empty(m, n, dtype=dtype, device=a._data.device), n
     else:
         ldo = _ld(out, m, n, "out")
-    index = _on_gpu(a.data, w.data, bias, out)
+    index = _on_gpu(a._data, w._data, bias, out)
     if m:
         _call(abi.rc_qgemm, index, C.byref(A), C.byref(W), None if bias is None else bias.data_ptr(), 1 if gelu else 0,
               out.data_ptr(), _dtype(out, "out"), ldo)
@@ -290,11 +306,11 @@ def quantize_int8(x: torch.Tensor, out: Optional[IntMatrix] = None) -> IntMatrix
             raise ValueError(f"{rows} x {cols} is too large")
         out = IntMatrix._new(rows, cols, index)
     else:
-        index = _on_gpu(x, out.data)
-        if out.data.shape != x.shape:
+        index = _on_gpu(x, out._data)
+        if (out._struct.rows, out._struct.cols) != shape:
             raise ValueError("out has another shape")
     if rows:
-        _call(abi.rc_quantize_int8, index, x.data_ptr(), dtype, ldx, C.byref(out._struct))
+        _call(abi.rc_quantize_int8, index, x.data_ptr(), dtype, ldx, C.byref(out.struct()))
     return out
 
 
@@ -302,7 +318,7 @@ def igemm(a: IntMatrix, w: IntMatrix, bias: Optional[torch.Tensor] = None, gelu:
           dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """act(a w^T + bias): a [m, k], w [n, k], bias float32 [n]; the result [m, n]
     in dtype (or in out).  The sum over k is exact."""
-    A, W = a._struct, w._struct
+    A, W = a.struct(), w.struct()
     m, n = A.rows, W.rows
     if bias is not None and (bias.dtype != _F32 or bias.shape != (n,) or not bias.is_contiguous()):
         raise ValueError(f"bias must be contiguous float32 [{n}]")
@@ -329,9 +345,9 @@ def qcache_store(cache: QuantCache, active: ActiveSet, k: torch.Tensor, v: torch
     ld = _ld(k, rows, cols, "k")
     if v.dtype != k.dtype or _ld(v, rows, cols, "v") != ld:
         raise ValueError("k and v must have one type and row stride")
-    index = _on_gpu(cache.data, k, v, active.idx, active.offsets)
+    index = _on_gpu(cache._data, k, v, active.idx, active.offsets)
     if rows:
-        _call(abi.rc_qcache_store, index, C.byref(cache._struct), C.byref(active.struct()), k.data_ptr(), v.data_ptr(), dtype, ld)
+        _call(abi.rc_qcache_store, index, C.byref(cache.struct()), C.byref(active.struct()), k.data_ptr(), v.data_ptr(), dtype, ld)
 
 
 def qcache_attention(cache: QuantCache, rows: ActiveSet, q: torch.Tensor, scale: Optional[float] = None,
@@ -351,9 +367,9 @@ def qcache_attention(cache: QuantCache, rows: ActiveSet, q: torch.Tensor, scale:
     elif out.dtype != torch.bfloat16:
         raise ValueError(f"out is {out.dtype}, not bfloat16")
     ldo = _ld(out, total, cols, "out")
-    index = _on_gpu(cache.data, q, out, key_len, rows.offsets)
+    index = _on_gpu(cache._data, q, out, key_len, rows.offsets)
     if total:
-        c, s = cache._struct, rows.struct()
+        c, s = cache.struct(), rows.struct()
         nbytes = abi.rc_qcache_attention_scratch_bytes(C.byref(c), C.byref(s))
         scratch = torch.empty(nbytes, dtype=_U8, device=q.device) if nbytes else None
         _call(abi.rc_qcache_attention, index, C.byref(c), C.byref(s), None if key_len is None else key_len.data_ptr(),

@@ -21,7 +21,7 @@ from typing import Optional, Union
 import torch
 
 from . import abi
-from .quant import _DTYPES, _F8, _F32, _I8, IntMatrix, QuantMatrix, _call, _dtype, _empty, _ld, _on_gpu
+from .quant import _DTYPES, _F8, _F32, _I8, IntMatrix, QuantMatrix, _call, _dtype, _empty, _ld, _on_gpu, _written
 from .runtime import ActiveSet
 
 __all__ = ["Norm", "norm_modulate", "residual_norm"]
@@ -132,6 +132,7 @@ def _run(x, h, gate, post, residual_scale, pre, scale, shift, rows, dtype, out):
         pgate, sgate = (0, 0) if gate is None else _vector(gate, cols, rows, index, "gate")
         ppost = 0 if post is None else _norm(post, cols, index, "post")
     ppre = pscale = sscale = pshift = sshift = pout = ldo = out_dtype = e4m3 = int8 = 0
+    written = () if out is None else (out,) if isinstance(out, torch.Tensor) else (out._data, out._scales)
     if pre is not None:
         ppre = _norm(pre, cols, index, "the norm")
         if scale is not None:
@@ -173,6 +174,9 @@ def _run(x, h, gate, post, residual_scale, pre, scale, shift, rows, dtype, out):
         _call(abi.rc_residual_norm, index, abi.norm_args(
             n, cols, x.data_ptr(), ldx, ph, ldh, x_dtype, h_dtype, ppost, ppre, residual_scale, sgate, sscale, sshift, pgate, pscale, pshift,
             0 if chains is None else C.addressof(chains), pout, ldo, out_dtype, e4m3, int8))
+        if h is not None:
+            _written(x)
+        _written(*written)
     return out
 
 

@@ -48,6 +48,8 @@ _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device
 # (0.8 us for a tensor of the current device, torch.empty 1.3)
 _empty_strided = getattr(getattr(getattr(torch._C, "_dynamo", None), "guards", None), "_empty_strided_cuda", None)
 
+_increment_version = torch.autograd.graph.increment_version
+
 
 def _empty(rows: int, cols: int, dtype: torch.dtype, index: int) -> torch.Tensor:
     """A new [rows][cols] tensor on GPU `index`."""
@@ -81,6 +83,12 @@ def _call(f, index: int, *args):
     else:
         with torch.cuda.device(index):
             f(*args, _raw_stream(index))
+
+
+def _written(*tensors: torch.Tensor) -> None:
+    """Tells autograd that kernels write them: a graph that saved one fails in its backward pass instead of using other values."""
+    for t in tensors:
+        _increment_version(t)
 
 
 def _ld(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
@@ -257,7 +265,8 @@ def quantize(x: torch.Tensor, block_rows: int = 1, out: Optional[QuantMatrix] = 
         raise ValueError(f"x is {tuple(x.shape)}, not [rows, cols]")
     rows, cols = x.shape
     ldx = cols if x.is_contiguous() else _ld(x, rows, cols, "x")
-    if out is None:
+    given = out is not None
+    if not given:
         index = _on_gpu(x)
         out = QuantMatrix.alloc(rows, cols, block_rows, x.device)
     else:
@@ -266,6 +275,8 @@ def quantize(x: torch.Tensor, block_rows: int = 1, out: Optional[QuantMatrix] = 
             raise ValueError("out has another shape or other blocks")
     if rows:
         _call(abi.rc_quantize, index, x.data_ptr(), dtype, ldx, C.byref(out.struct()))
+        if given:
+            _written(out._data, out._scales)
     return out
 
 
@@ -277,7 +288,8 @@ def qgemm(a: QuantMatrix, w: QuantMatrix, bias: Optional[torch.Tensor] = None, g
     m, n = A.rows, W.rows
     if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,) or not bias.is_contiguous()):
         raise ValueError(f"bias must be contiguous float32 [{n}]")
-    if out is None:
+    given = out is not None
+    if not given:
         if dtype not in _DTYPES:
             raise ValueError(f"dtype {dtype} is not float32 or bfloat16")
         out, ldo = torch.empty(m, n, dtype=dtype, device=a._data.device), n
@@ -287,6 +299,8 @@ def qgemm(a: QuantMatrix, w: QuantMatrix, bias: Optional[torch.Tensor] = None, g
     if m:
         _call(abi.rc_qgemm, index, C.byref(A), C.byref(W), None if bias is None else bias.data_ptr(), 1 if gelu else 0,
               out.data_ptr(), _dtype(out, "out"), ldo)
+        if given:
+            _written(out)
     return out
 
 
@@ -300,7 +314,8 @@ def quantize_int8(x: torch.Tensor, out: Optional[IntMatrix] = None) -> IntMatrix
         raise ValueError(f"x is {tuple(shape)}, not [rows, cols]")
     rows, cols = shape
     ldx = cols if x.is_contiguous() else _ld(x, rows, cols, "x")
-    if out is None:
+    given = out is not None
+    if not given:
         index = _on_gpu(x)
         if rows >> 31 or cols >> 31:
             raise ValueError(f"{rows} x {cols} is too large")
@@ -311,6 +326,8 @@ def quantize_int8(x: torch.Tensor, out: Optional[IntMatrix] = None) -> IntMatrix
             raise ValueError("out has another shape")
     if rows:
         _call(abi.rc_quantize_int8, index, x.data_ptr(), dtype, ldx, C.byref(out.struct()))
+        if given:
+            _written(out._data, out._scales)
     return out
 
 
@@ -322,7 +339,8 @@ def igemm(a: IntMatrix, w: IntMatrix, bias: Optional[torch.Tensor] = None, gelu:
     m, n = A.rows, W.rows
     if bias is not None and (bias.dtype != _F32 or bias.shape != (n,) or not bias.is_contiguous()):
         raise ValueError(f"bias must be contiguous float32 [{n}]")
-    if out is None:
+    given = out is not None
+    if not given:
         code = _DTYPES.get(dtype)
         if code is None:
             raise ValueError(f"dtype {dtype} is not float32 or bfloat16")
@@ -334,6 +352,8 @@ def igemm(a: IntMatrix, w: IntMatrix, bias: Optional[torch.Tensor] = None, gelu:
     if m:
         _call(abi.rc_igemm, index, C.byref(A), C.byref(W), None if bias is None else bias.data_ptr(), 1 if gelu else 0,
               out.data_ptr(), code, ldo)
+        if given:
+            _written(out)
     return out
 
 
@@ -348,6 +368,7 @@ def qcache_store(cache: QuantCache, active: ActiveSet, k: torch.Tensor, v: torch
     index = _on_gpu(cache._data, k, v, active.idx, active.offsets)
     if rows:
         _call(abi.rc_qcache_store, index, C.byref(cache.struct()), C.byref(active.struct()), k.data_ptr(), v.data_ptr(), dtype, ld)
+        _written(cache._data, cache._scales)
 
 
 def qcache_attention(cache: QuantCache, rows: ActiveSet, q: torch.Tensor, scale: Optional[float] = None,
@@ -362,7 +383,8 @@ def qcache_attention(cache: QuantCache, rows: ActiveSet, q: torch.Tensor, scale:
     ldq = cols if q.shape == (total, cols) and q.is_contiguous() else _ld(q, total, cols, "q")
     if key_len is not None and (key_len.dtype != torch.int32 or key_len.shape != (cache.batch,) or not key_len.is_contiguous()):
         raise ValueError(f"key_len must be contiguous int32 [{cache.batch}]")
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty(total, cols, dtype=torch.bfloat16, device=q.device)
     elif out.dtype != torch.bfloat16:
         raise ValueError(f"out is {out.dtype}, not bfloat16")
@@ -375,4 +397,6 @@ def qcache_attention(cache: QuantCache, rows: ActiveSet, q: torch.Tensor, scale:
         _call(abi.rc_qcache_attention, index, C.byref(c), C.byref(s), None if key_len is None else key_len.data_ptr(),
               q.data_ptr(), ldq, _SCALE if scale is None else float(scale), out.data_ptr(), ldo,
               scratch.data_ptr() if nbytes else None, nbytes)
+        if given:
+            _written(out)
     return out

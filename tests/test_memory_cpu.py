@@ -3,20 +3,11 @@ tensors in host memory, which nothing reads)."""
 import pytest
 import torch
 
+from _host_calls import calls  # noqa: F401  (a fixture)
 from paper_2608_29809_amd import norm, quant
 from paper_2608_29809_amd.runtime import ActiveSet
 
 F8 = torch.float8_e4m3fn
-
-
-@pytest.fixture
-def calls(monkeypatch):
-    """Host tensors pass for those of GPU 0, and calls are listed instead of made."""
-    made = []
-    for module in (quant, norm):
-        monkeypatch.setattr(module, "_on_gpu", lambda *tensors: -1)
-        monkeypatch.setattr(module, "_call", lambda f, index, *args: made.append(f.__name__))
-    return made
 
 
 def rows(n, cols=16):

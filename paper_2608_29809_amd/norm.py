@@ -11,7 +11,8 @@ only; every computation is a call into libregioncache.so.
 scale, shift and gate are one vector, or one for each chain with the chains'
 row ranges in `rows`.  Results are bfloat16 or float32 tensors, for dtype
 torch.float8_e4m3fn a QuantMatrix and for torch.int8 an IntMatrix.  Calls go to
-the current stream of their tensors' device.
+the current stream of their tensors' device.  There are no gradients: where they
+are recorded, tensors that require one are refused; a norm's weights are constants.
 """
 from __future__ import annotations
 
@@ -21,7 +22,7 @@ from typing import Optional, Union
 import torch
 
 from . import abi
-from .quant import _DTYPES, _F8, _F32, _I8, IntMatrix, QuantMatrix, _call, _dtype, _empty, _ld, _on_gpu, _written
+from .quant import _DTYPES, _F8, _F32, _I8, IntMatrix, QuantMatrix, _call, _dtype, _empty, _ld, _no_gradient, _on_gpu, _written
 from .runtime import ActiveSet
 
 __all__ = ["Norm", "norm_modulate", "residual_norm"]
@@ -188,6 +189,7 @@ def norm_modulate(x: torch.Tensor, norm: Norm, scale: Optional[torch.Tensor] = N
     read)."""
     if norm is None:
         raise ValueError("norm is None")
+    _no_gradient("norm_modulate", x, scale, shift, getattr(out, "_scales", out))
     return _run(x, None, None, None, 1.0, norm, scale, shift, rows, dtype, out)
 
 
@@ -201,4 +203,5 @@ def residual_norm(x: torch.Tensor, h: torch.Tensor, gate: Optional[torch.Tensor]
     float32 or bfloat16; x, h and out do not overlap; gate like scale and shift."""
     if h is None:
         raise ValueError("h is None")
+    _no_gradient("residual_norm", x, h, gate, scale, shift, getattr(out, "_scales", out))
     return _run(x, h, gate, post, residual_scale, pre, scale, shift, rows, dtype, out)

@@ -91,6 +91,14 @@ def _written(*tensors: torch.Tensor) -> None:
         _increment_version(t)
 
 
+def _no_gradient(name: str, *tensors: Optional[torch.Tensor]) -> None:
+    """Refuses tensors through which autograd would expect a gradient: the operators have none."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{name} has no gradient: call it under torch.no_grad() or with detached tensors")
+
+
 def _ld(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
     """Elements between the rows of a [rows][cols] tensor whose rows are contiguous."""
     if t.shape != (rows, cols):
@@ -307,7 +315,8 @@ def qgemm(a: QuantMatrix, w: QuantMatrix, bias: Optional[torch.Tensor] = None, g
 def quantize_int8(x: torch.Tensor, out: Optional[IntMatrix] = None) -> IntMatrix:
     """x [rows, cols] float32 or bfloat16, cols a multiple of 16, in int8 with a
     scale for each row: a weight's output channels, an activation's tokens.  A
-    row that holds a value that is not finite gets the scale NaN."""
+    row that holds a value that is not finite gets the scale NaN.  Nothing of the
+    result has a gradient."""
     dtype = _dtype(x, "x")
     shape = x.shape
     if len(shape) != 2:
@@ -334,7 +343,9 @@ def quantize_int8(x: torch.Tensor, out: Optional[IntMatrix] = None) -> IntMatrix
 def igemm(a: IntMatrix, w: IntMatrix, bias: Optional[torch.Tensor] = None, gelu: bool = False,
           dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """act(a w^T + bias): a [m, k], w [n, k], bias float32 [n]; the result [m, n]
-    in dtype (or in out).  The sum over k is exact."""
+    in dtype (or in out).  The sum over k is exact.  There is no gradient: tensors
+    that require one are refused where they are recorded."""
+    _no_gradient("igemm", a._scales, w._scales, bias, out)
     A, W = a.struct(), w.struct()
     m, n = A.rows, W.rows
     if bias is not None and (bias.dtype != _F32 or bias.shape != (n,) or not bias.is_contiguous()):

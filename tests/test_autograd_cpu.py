@@ -14,8 +14,8 @@ def rows(n=40, cols=16, **more):
     return torch.zeros(n, cols, **more)
 
 
-def imat():
-    return quant.IntMatrix(torch.zeros(40, 16, dtype=torch.int8), torch.ones(40))
+def imat(scales=None):
+    return quant.IntMatrix(torch.zeros(40, 16, dtype=torch.int8), torch.ones(40) if scales is None else scales)
 
 
 def qmat(block_rows=1):
@@ -77,3 +77,39 @@ def test_inference_tensors(calls):
         norm.residual_norm(x, rows(), pre=N(), out=rows())
     norm.residual_norm(x, rows())
     assert len(calls) == 2
+
+
+def takes():
+    """A call of tensors, and those tensors, each of which autograd would expect a gradient through."""
+    v = [torch.zeros(16) for _ in range(3)]
+    return {
+        "norm_modulate": (lambda x, scale, shift, out: norm.norm_modulate(x, N(), scale, shift, out=out), [rows(), v[0], v[1], rows()]),
+        "residual_norm": (lambda x, h, gate, scale, shift, out: norm.residual_norm(x, h, gate, pre=N(), scale=scale, shift=shift, out=out),
+                          [rows(), rows(), *v, rows()]),
+        "norm_modulate to int8": (lambda x, scales: norm.norm_modulate(x, N(), out=imat(scales)), [rows(), torch.ones(40)]),
+        "igemm": (lambda a, w, bias, out: quant.igemm(imat(a), imat(w), bias, out=out), [torch.ones(40), torch.ones(40), torch.zeros(40), rows(40, 40)]),
+    }
+
+
+@pytest.mark.parametrize("name", takes())
+def test_gradients_are_refused(calls, name):
+    """A tensor that requires a gradient, a leaf or a result, is refused while gradients are recorded, and only then."""
+    call, tensors = takes()[name]
+    for i in range(len(tensors)):
+        leaf = [t.clone().requires_grad_(k == i) for k, t in enumerate(tensors)]
+        result = [t.clone() for t in tensors]
+        result[i] = tensors[i].clone().requires_grad_() * 2
+        for given in (leaf, result):
+            with pytest.raises(ValueError, match=f"{name.split()[0]} has no gradient"):
+                call(*given)
+            assert not calls
+            for off in (torch.no_grad, torch.inference_mode):
+                with off():
+                    call(*given)
+            call(*[t.detach() for t in given])
+            assert len(calls) == 3
+            calls.clear()
+    norm.norm_modulate(rows(), N(weight=torch.nn.Parameter(torch.zeros(16))), out=rows())  # (a norm's weights are constants)
+    with torch.no_grad():
+        quant.quantize_int8(rows().requires_grad_(), out=imat())
+    quant.quantize_int8(rows().requires_grad_(), out=imat())  # (integers, of which none is expected)

@@ -97,8 +97,10 @@ template <int L> __device__ __forceinline__ float lanes_sum(float v) {
 }
 constexpr int kNormWaves = 16;  // most that share a row
 template <typename H> constexpr bool kUpdate = !std::is_same<H, void>::value;  // h of type H, or none
-// Waves of a SIMD that the registers leave: 6 (80 registers) do without spills where a wave or
-// more share a row, one unit each; not 16 lanes' chains, which differ within a wave, nor, at 4, theirs with an update.
+// Waves of a SIMD that the registers leave: 6 (80 registers) where a wave or more share a row, one
+// unit each; not 16 lanes' chains, which differ within a wave, nor, at 4, theirs with an update.  No
+// vector register is spilled but two of <0, 1, NF_ANY, float, void>; scalar ones are, to lanes of a
+// vector register: up to 22 with an update, of rows under eight columns 42, and 109 to 123 with one.
 template <int L, int U, typename H> constexpr int kNormResident = L == 16 ? (kUpdate<H> ? 3 : 4) : U == 1 && !kUpdate<H> ? 6 : 4;
 
 // One pass over the data: a row stays in the registers of the threads that share

@@ -45,9 +45,10 @@ _SCALE = 1.0 / math.sqrt(HEAD_DIM)
 # PyTorch; where they are missing the public ones serve.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-# (0.8 us for a tensor of the current device, torch.empty 1.3)
+# (0.8 us for a tensor of the current device, torch.empty 1.3.  Results are made past Python's
+# dispatch, so modes that replace or watch torch.empty do not see them, and past the filling
+# of new memory that deterministic algorithms ask for: kernels write all of a result.)
 _empty_strided = getattr(getattr(getattr(torch._C, "_dynamo", None), "guards", None), "_empty_strided_cuda", None)
-
 _increment_version = torch.autograd.graph.increment_version
 
 

@@ -22,7 +22,7 @@ from typing import Optional, Union
 import torch
 
 from . import abi
-from .quant import _DTYPES, _F8, _F32, _I8, IntMatrix, QuantMatrix, _call, _dtype, _empty, _ld, _no_gradient, _on_gpu, _written
+from .quant import _DTYPES, _F8, _F32, _I8, IntMatrix, QuantMatrix, _call, _dtype, _empty, _grad_enabled, _ld, _no_gradient, _on_gpu, _written
 from .runtime import ActiveSet
 
 __all__ = ["Norm", "norm_modulate", "residual_norm"]
@@ -117,6 +117,13 @@ def _norm(norm: Norm, cols: int, index: int, what: str) -> int:
 
 
 def _run(x, h, gate, post, residual_scale, pre, scale, shift, rows, dtype, out):
+    written = () if h is None else (x,)
+    if out is not None:
+        written += (out,) if isinstance(out, torch.Tensor) else (out._data, out._scales)
+    if _grad_enabled() and (x.requires_grad or h is not None and h.requires_grad or gate is not None and gate.requires_grad
+                            or scale is not None and scale.requires_grad or shift is not None and shift.requires_grad
+                            or written and written[-1].requires_grad):
+        raise _no_gradient("norm_modulate" if h is None else "residual_norm")
     shape = x.shape
     if len(shape) != 2:
         raise ValueError(f"x is {tuple(shape)}, not [rows, cols]")
@@ -133,7 +140,6 @@ def _run(x, h, gate, post, residual_scale, pre, scale, shift, rows, dtype, out):
         pgate, sgate = (0, 0) if gate is None else _vector(gate, cols, rows, index, "gate")
         ppost = 0 if post is None else _norm(post, cols, index, "post")
     ppre = pscale = sscale = pshift = sshift = pout = ldo = out_dtype = e4m3 = int8 = 0
-    written = () if out is None else (out,) if isinstance(out, torch.Tensor) else (out._data, out._scales)
     if pre is not None:
         ppre = _norm(pre, cols, index, "the norm")
         if scale is not None:
@@ -175,9 +181,8 @@ def _run(x, h, gate, post, residual_scale, pre, scale, shift, rows, dtype, out):
         _call(abi.rc_residual_norm, index, abi.norm_args(
             n, cols, x.data_ptr(), ldx, ph, ldh, x_dtype, h_dtype, ppost, ppre, residual_scale, sgate, sscale, sshift, pgate, pscale, pshift,
             0 if chains is None else C.addressof(chains), pout, ldo, out_dtype, e4m3, int8))
-        if h is not None:
-            _written(x)
-        _written(*written)
+        if written:
+            _written(written)
     return out
 
 
@@ -189,7 +194,6 @@ def norm_modulate(x: torch.Tensor, norm: Norm, scale: Optional[torch.Tensor] = N
     read)."""
     if norm is None:
         raise ValueError("norm is None")
-    _no_gradient("norm_modulate", x, scale, shift, getattr(out, "_scales", out))
     return _run(x, None, None, None, 1.0, norm, scale, shift, rows, dtype, out)
 
 
@@ -203,5 +207,4 @@ def residual_norm(x: torch.Tensor, h: torch.Tensor, gate: Optional[torch.Tensor]
     float32 or bfloat16; x, h and out do not overlap; gate like scale and shift."""
     if h is None:
         raise ValueError("h is None")
-    _no_gradient("residual_norm", x, h, gate, scale, shift, getattr(out, "_scales", out))
     return _run(x, h, gate, post, residual_scale, pre, scale, shift, rows, dtype, out)

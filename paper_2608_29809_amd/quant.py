@@ -49,7 +49,10 @@ _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device
 # dispatch, so modes that replace or watch torch.empty do not see them, and past the filling
 # of new memory that deterministic algorithms ask for: kernels write all of a result.)
 _empty_strided = getattr(getattr(getattr(torch._C, "_dynamo", None), "guards", None), "_empty_strided_cuda", None)
-_increment_version = torch.autograd.graph.increment_version
+# Tells autograd that kernels write tensors (one or a tuple): a graph that saved one fails
+# in its backward pass instead of using other values.
+_written = torch.autograd.graph.increment_version
+_grad_enabled = torch.is_grad_enabled
 
 
 def _empty(rows: int, cols: int, dtype: torch.dtype, index: int) -> torch.Tensor:
@@ -86,18 +89,9 @@ def _call(f, index: int, *args):
             f(*args, _raw_stream(index))
 
 
-def _written(*tensors: torch.Tensor) -> None:
-    """Tells autograd that kernels write them: a graph that saved one fails in its backward pass instead of using other values."""
-    for t in tensors:
-        _increment_version(t)
-
-
-def _no_gradient(name: str, *tensors: Optional[torch.Tensor]) -> None:
-    """Refuses tensors through which autograd would expect a gradient: the operators have none."""
-    if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise ValueError(f"{name} has no gradient: call it under torch.no_grad() or with detached tensors")
+def _no_gradient(name: str) -> ValueError:
+    """Of a tensor through which autograd would expect a gradient: the operators have none."""
+    return ValueError(f"{name} has no gradient: call it under torch.no_grad() or with detached tensors")
 
 
 def _ld(t: torch.Tensor, rows: int, cols: int, what: str) -> int:
@@ -117,31 +111,19 @@ class _InMemory:
     sizes, made once: where the tensors were given other memory since (set_,
     resize_, .data) it is refused."""
 
-    __slots__ = ("_data", "_scales", "_struct", "_memory")  # (_memory: None while nobody else has seen the tensors)
+    __slots__ = ("_data", "_scales", "_struct", "_at_data", "_at_scales")
 
-    def _seen(self) -> None:
-        data, scales = self._data, self._scales
-        of_data, of_scales = data.untyped_storage(), scales.untyped_storage()  # (kept: what the structure points to is not freed)
-        self._memory = data.data_ptr(), of_data, of_data.nbytes(), scales.data_ptr(), of_scales, of_scales.nbytes()
+    def _hold(self, data: torch.Tensor, scales: torch.Tensor, kind, *sizes) -> None:
+        self._data, self._scales = data, scales
+        self._at_data, self._at_scales = at_data, at_scales = data.data_ptr(), scales.data_ptr()
+        self._struct = kind(at_data, at_scales, *sizes)
 
-    @property
-    def data(self) -> torch.Tensor:
-        if self._memory is None:
-            self._seen()
-        return self._data
-
-    @property
-    def scales(self) -> torch.Tensor:
-        if self._memory is None:
-            self._seen()
-        return self._scales
+    data = property(lambda self: self._data)
+    scales = property(lambda self: self._scales)
 
     def struct(self):
-        if self._memory is not None:
-            data, of_data, data_bytes, scales, of_scales, scales_bytes = self._memory
-            if (self._data.data_ptr() != data or of_data.nbytes() != data_bytes or self._scales.data_ptr() != scales
-                    or of_scales.nbytes() != scales_bytes):
-                raise ValueError(f"the memory of a {type(self).__name__}'s tensors was exchanged or resized")
+        if self._data.data_ptr() != self._at_data or self._scales.data_ptr() != self._at_scales:
+            raise ValueError(f"the memory of a {type(self).__name__}'s tensors was exchanged or resized")
         return self._struct
 
 
@@ -164,10 +146,8 @@ class QuantMatrix(_InMemory):
             raise ValueError(f"scales {tuple(scales.shape)} do not cover data {tuple(data.shape)} (row blocks padded to 16)")
         _on_gpu(data, scales)
         ld = cols if data.is_contiguous() else _ld(data, rows, cols, "data")
-        self._data, self._scales, self._block_rows = data, scales, block_rows
-        self._seen()
-        self._struct = abi.rc_qmat(data.data_ptr(), scales.data_ptr(), ld, rows, cols,
-                                   row_blocks if col_blocks == 1 else scales.stride(0), block_rows)
+        self._block_rows = block_rows
+        self._hold(data, scales, abi.rc_qmat, ld, rows, cols, row_blocks if col_blocks == 1 else scales.stride(0), block_rows)
 
     block_rows = property(lambda self: self._block_rows)
 
@@ -180,10 +160,9 @@ class QuantMatrix(_InMemory):
         m = cls.__new__(cls)
         row_blocks = -(-rows // block_rows)
         row_blocks += -row_blocks % 16
-        m._data = data = torch.empty(rows, cols, dtype=_F8, device=device)
-        m._scales = scales = torch.empty(-(-cols // BLOCK), row_blocks, dtype=_U8, device=device)
-        m._block_rows, m._memory = block_rows, None
-        m._struct = abi.rc_qmat(data.data_ptr(), scales.data_ptr(), cols, rows, cols, row_blocks, block_rows)
+        m._block_rows = block_rows
+        m._hold(torch.empty(rows, cols, dtype=_F8, device=device), torch.empty(-(-cols // BLOCK), row_blocks, dtype=_U8, device=device),
+                abi.rc_qmat, cols, rows, cols, row_blocks, block_rows)
         return m
 
 
@@ -203,10 +182,7 @@ class IntMatrix(_InMemory):
         if rows >> 31 or cols >> 31:
             raise ValueError(f"{rows} x {cols} is too large")
         _on_gpu(data, scales)
-        self._data, self._scales = data, scales
-        self._seen()
-        ld = cols if data.is_contiguous() else _ld(data, rows, cols, "data")
-        self._struct = abi.rc_imat(data.data_ptr(), scales.data_ptr(), ld, rows, cols)
+        self._hold(data, scales, abi.rc_imat, cols if data.is_contiguous() else _ld(data, rows, cols, "data"), rows, cols)
 
     @classmethod
     def alloc(cls, rows: int, cols: int, device="cuda") -> "IntMatrix":
@@ -223,8 +199,7 @@ class IntMatrix(_InMemory):
     @classmethod
     def _of(cls, data: torch.Tensor, scales: torch.Tensor, rows: int, cols: int) -> "IntMatrix":
         m = cls.__new__(cls)
-        m._data, m._scales, m._memory = data, scales, None
-        m._struct = abi.rc_imat(data.data_ptr(), scales.data_ptr(), cols, rows, cols)
+        m._hold(data, scales, abi.rc_imat, cols, rows, cols)
         return m
 
 
@@ -249,11 +224,8 @@ class QuantCache(_InMemory):
         if not (data.is_contiguous() or data[0].is_contiguous()) or not (scales.is_contiguous() or scales[0].is_contiguous()):
             raise ValueError("a chain of the cache must be contiguous")
         _on_gpu(data, scales)
-        self._data, self._scales = data, scales
-        self._seen()
         self.batch, self.heads, self.tokens = batch, heads, blocks * KEY_BLOCK
-        self._struct = abi.rc_qcache(data.data_ptr(), scales.data_ptr(), data.stride(0), scales.stride(0), batch, heads,
-                                     self.tokens)
+        self._hold(data, scales, abi.rc_qcache, data.stride(0), scales.stride(0), batch, heads, self.tokens)
 
     @classmethod
     def alloc(cls, batch: int, heads: int, tokens: int, device="cuda") -> "QuantCache":
@@ -285,7 +257,7 @@ def quantize(x: torch.Tensor, block_rows: int = 1, out: Optional[QuantMatrix] = 
     if rows:
         _call(abi.rc_quantize, index, x.data_ptr(), dtype, ldx, C.byref(out.struct()))
         if given:
-            _written(out._data, out._scales)
+            _written((out._data, out._scales))
     return out
 
 
@@ -337,7 +309,7 @@ def quantize_int8(x: torch.Tensor, out: Optional[IntMatrix] = None) -> IntMatrix
     if rows:
         _call(abi.rc_quantize_int8, index, x.data_ptr(), dtype, ldx, C.byref(out.struct()))
         if given:
-            _written(out._data, out._scales)
+            _written((out._data, out._scales))
     return out
 
 
@@ -346,7 +318,9 @@ def igemm(a: IntMatrix, w: IntMatrix, bias: Optional[torch.Tensor] = None, gelu:
     """act(a w^T + bias): a [m, k], w [n, k], bias float32 [n]; the result [m, n]
     in dtype (or in out).  The sum over k is exact.  There is no gradient: tensors
     that require one are refused where they are recorded."""
-    _no_gradient("igemm", a._scales, w._scales, bias, out)
+    if _grad_enabled() and (a._scales.requires_grad or w._scales.requires_grad or bias is not None and bias.requires_grad
+                            or out is not None and out.requires_grad):
+        raise _no_gradient("igemm")
     A, W = a.struct(), w.struct()
     m, n = A.rows, W.rows
     if bias is not None and (bias.dtype != _F32 or bias.shape != (n,) or not bias.is_contiguous()):
@@ -380,7 +354,7 @@ def qcache_store(cache: QuantCache, active: ActiveSet, k: torch.Tensor, v: torch
     index = _on_gpu(cache._data, k, v, active.idx, active.offsets)
     if rows:
         _call(abi.rc_qcache_store, index, C.byref(cache.struct()), C.byref(active.struct()), k.data_ptr(), v.data_ptr(), dtype, ld)
-        _written(cache._data, cache._scales)
+        _written((cache._data, cache._scales))
 
 
 def qcache_attention(cache: QuantCache, rows: ActiveSet, q: torch.Tensor, scale: Optional[float] = None,

@@ -4,10 +4,15 @@
 // as it suits; they are rounded once, to float32, before the two scales.
 //
 // Two kinds of tiles: those of rc_qgemm_tiles.h for any shape and type, and those of
-// igemm_step_kernel below.  With launches, us: 1 x 4608 x 1152 4.3; 400 x 4608 x 1152 6.9;
-// 723 x 1152 x 4608 10.0; 723 x 4608 x 1152 with GELU 8.7; 4096 x 1152 x 4608 24; 4096 x 4608
-// x 1152 with GELU 30; 16384 x 4608 x 1152 88, 105 with GELU; 16384 x 1152 x 4608 80;
-// 8192 x 8192 x 8192 375, 2.9 POP/s (PyTorch's int8 product 520).
+// igemm_step_kernel below.  In a captured graph, one call behind the other, us: 1 x 4608 x
+// 1152 3.5; 400 x 4608 x 1152 5.7; 723 x 1152 x 4608 9.5; 723 x 4608 x 1152 with GELU 8.2; 4096 x
+// 1152 x 4608 24; 4096 x 4608 x 1152 with GELU 30; 16384 x 4608 x 1152 87, 100 with GELU; 16384 x
+// 1152 x 4608 80; 8192 x 8192 x 8192 365, 3.0 POP/s (PyTorch's int8 product 520).
+//
+// float32 results take the tiles of rc_qgemm_tiles.h up to 128 x 128 only: the others' epilogues
+// pack bfloat16, which the steps and a next quantisation take.  The same calls: 400 x 4608 x 1152
+// 8.1; 723 x 1152 x 4608 11.2; 723 x 4608 x 1152 10.8 (bfloat16 7.4); 4096 x 1152 x 4608 34; 16384 x
+// 4608 x 1152 131, whose 302 MB of results alone are 59 at a copy's rate; 8192 x 8192 x 8192 546.
 #include "rc_common.h"
 #include "rc_int8.h"
 #include "rc_launch.h"

@@ -24,8 +24,8 @@ template <> struct I8Raw<bf16> {
 // it, eight columns times U each, from the maximum to the rounding: sixteen lanes
 // (L = 16), a wave (L = 64) or a workgroup of as many waves as it takes (L = 0).
 // Columns behind the last are copies of the last eight and not stored.  Bound by
-// its bytes for many rows: 16384 x 4608 bfloat16 values 45 us (5.0 TB/s), 4096 x 4608
-// 14.4, 4608 x 1152 float32 6.7; by latency for few: 723 x 4608 5.2, of which a
+// its bytes for many rows: 16384 x 4608 bfloat16 values 42-45 us (5.0-5.4 TB/s), 4096 x 4608
+// 12.5-14.5, 4608 x 1152 float32 6.5; by latency for few: 723 x 4608 4.6, of which a
 // launch is 3.  Rows one after another by fewer workgroups, the next one sent for
 // ahead, were slower (4096 x 4608: 18.7 us), as was a unit a thread (18.6): what the
 // threads of a row do once, the exchanges, is spread over more values.

@@ -115,12 +115,13 @@ template <int L, int U, typename H> constexpr int kNormResident = L == 16 ? (kUp
 // sums of squares do.
 //
 // Bound by its bytes for many rows: an update of 16384 x 1152 float32 values by
-// bfloat16 ones with the next norm 49 us (4.6 TB/s), a norm of them to bfloat16 24.5; by
-// instructions and the exchanges' waits where results are 8 bits (4096 x 4608
-// bfloat16 to e4m3 15.3 us, 3.7 TB/s; to int8 23); by latency for few rows (723 x 1152
-// to int8 4.9 us, with an update 5.2; one row 2.7, a launch).  One row a workgroup
-// without `chunk` loads the vectors for each (16384 x 1152: 30 us instead of 24.5); two
-// rows at a time, whose exchanges are one, were slower (26).
+// bfloat16 ones with the next norm 49 us (4.6 TB/s), alone 41; a norm of them to bfloat16
+// 22.5 (5.0 TB/s); by instructions and the exchanges' waits where results are 8 bits (4096 x
+// 4608 bfloat16 to e4m3 17-18 us, to int8 21-22.5; with an update to e4m3 28, but to int8 47:
+// one workgroup a CU, which waits at two exchanges a row); by latency for few rows (723 x
+// 1152 to int8 4.5 us, with an update 5.4; one row 2.6, a launch).  One row a workgroup
+// without `chunk` loads the vectors for each (16384 x 1152: 30 us where it then took 24.5 with
+// it); two rows at a time, whose exchanges are one, were slower (26).
 template <int L, int U, int FORM, typename X, typename H>
 __global__ __launch_bounds__(L ? 256 : 1024, (kNormResident<L, U, H>)) void norm_kernel(NormArgs a, int chunk) {
   constexpr bool RES = kUpdate<H>;

@@ -71,7 +71,7 @@ class Norm:
             return None
         _intact(held, "a norm's weights")
         memory, start, _ = held
-        return torch.empty(0, dtype=_F32, device=memory.device).set_(memory, ((address or 0) - start) // 4, (self._cols,))
+        return torch.empty(0, dtype=_F32, device=memory.device).set_(memory, max(0, (address or 0) - start) // 4, (self._cols,))
 
     # (read-only: the C structure is made once)
     kind = property(lambda self: self._kind)

@@ -173,6 +173,11 @@ def test_memory_of_weights(given, part):
                 getattr(n, part)
 
 
+def test_weights_without_values():
+    for w in (torch.zeros(0), torch.zeros(64)[32:32], torch.zeros(64)[:0]):
+        assert norm.Norm(weight=w).weight.shape == (0,)
+
+
 def test_weights_elsewhere():
     n = norm.Norm(weight=torch.zeros(8))
     assert norm._norm(n, 8, -1, "post")

@@ -129,7 +129,7 @@ def _load():
         raise ImportError(f"{LIB_PATH} is missing: build it with paper_2608_29809_amd/build.py "
                           "(or __graft_entry__.build())")
     lib = C.CDLL(LIB_PATH)
-    if os.path.isdir(build.CSRC):  # (beside its sources: structures that do not match them would be read as pointers)
+    if os.path.isdir(build.CSRC) and os.path.exists(build.HEADER):  # (structures that do not match would be read as pointers)
         of = getattr(lib, "rc_source_digest", None)
         if of is not None:
             of.restype, of.argtypes = C.c_char_p, []

@@ -84,3 +84,9 @@ def test_failed_build_leaves_no_library(monkeypatch, tmp_path, fails):
     with pytest.raises(RuntimeError):
         build.build()
     assert not os.path.exists(build.LIB)
+
+
+@pytest.mark.parametrize("part", ["CSRC", "HEADER"])
+def test_library_without_its_sources_is_loaded(monkeypatch, tmp_path, part):
+    monkeypatch.setattr(build, part, str(tmp_path / "missing"))
+    assert abi._load().rc_source_digest()
